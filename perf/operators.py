@@ -165,6 +165,7 @@ def _moe_inputs(c, seed):
         x["residual"] = _normal((T, d), 4.0, g, dt)
         x["delta"] = _normal((T, d), 1.0, g, torch.float32)
         x["norm_weight"] = (1.0 + _normal((1, d), 0.1, g)).to(dt)
+        x["residual_out"] = _normal((T, d), 1.0, g, dt)
     else:
         x["h"] = _normal((T, d), 1.0, g, dt)
         if c["act"] == "mx8":
@@ -203,7 +204,7 @@ def prepare(case, seed):
         s["h"] = torch.empty((rows, d), dtype=dt, device="cuda") if c.get("outh") else None
         s["residual_out"] = torch.empty((rows, d), dtype=dt, device="cuda") if c["op"] == "norm" else None
     elif c["op"] == "block":
-        s["residual_out"] = torch.empty_like(x["residual"])
+        s["residual_out"] = x["residual_out"]
     if own and c["op"] in ("layer", "block"):
         from paper_2609_04895_amd import cmoe as B
         cfg = B.make_moe_config(1, c["N"], c["K"], c["d"], c["F"], c["T"], B.CMOE_BF16 if c["dtype"] == "bf16" else B.CMOE_F32,
@@ -317,6 +318,7 @@ def _run_plain(s):
     if x["n"] is not None:
         live = (torch.arange(c["T"], device="cuda") < x["n"]).unsqueeze(1)
         y, sel, gates = torch.where(live, y, x["y"]), torch.where(live, sel, x["selected"]), torch.where(live, gates, x["gates"])
+        r = None if r is None else torch.where(live, r, x["residual_out"])
     return _outputs(c, y, sel, gates, r, None, None, None)
 
 
@@ -425,6 +427,8 @@ def exact(case, seed):
     if x["n"] is not None:
         n = T - c["pad"]
         y[n:], gates[n:], sel[n:] = x["y"][n:].double(), x["gates"][n:].double(), x["selected"][n:]
+        if c["op"] == "block":
+            r[n:] = x["residual_out"][n:].double()
     out = {"y": y, "selected": sel, "gates": gates}
     if c["op"] == "block":
         out["residual"] = r
