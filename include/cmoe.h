@@ -334,6 +334,139 @@ cmoe_status cmoe_concentration(cmoe_handle* hd, int32_t top_m, double* out4);
  * nothing. */
 cmoe_status cmoe_read_probe(const void* src, int64_t bytes, int32_t reps, double* gbps);
 
+/* ------------------------------------------------------------------------
+ * Operators around an MoE layer without an expert cache: the layer for a few
+ * tokens straight from the weight pool, and what stands between two layers.
+ * They share the conventions above (status, cmoe_last_error, caller-owned
+ * buffers and streams, no hipMalloc) and are asynchronous on their stream;
+ * they may be captured into a HIP graph.  Two calls that overlap in time must
+ * not share a handle (a layer's workspace belongs to its handle; handles may
+ * share weights): this holds for replayed graphs too.
+ *
+ * 8-bit values: e4m3 numbers (one byte each) with one power-of-two scale 2^E for
+ * every 32 consecutive values of a row, kept as the byte E + 127.  E is the
+ * smallest exponent, -127 at least, with max |v| <= 448 2^E, so that nothing
+ * saturates; each value is rounded once, to nearest even.  A block that holds an
+ * infinity or a NaN gets the byte 255 and NaN (0x7F) in all its places.
+ */
+
+/* Residual addition and root-mean-square norm of `rows` rows of d values:
+ *   r = fl(residual + delta)              (residual, without a delta)
+ *   h = r / sqrt(mean(r^2) + eps) * weight
+ * r is rounded to dtype, stored to residual_out and normalised as stored; sums
+ * are fp32; h is rounded once, to dtype (h) and to 8 bits (h8, h8_scale).
+ * Between two layer steps delta is the y of cmoe_step or cmoe_moe_layer, and h
+ * the next layer's hidden states: strides let both be rows of [S][L][d].
+ * Strides count values (h8 and h8_scale: bytes) and are at least the row.
+ * residual_out may be residual itself (same stride); no other output may
+ * overlap an input or another output.  At least one output is given. */
+typedef struct {
+    int32_t rows, d;            /* rows <= 2^21                                    */
+    int32_t dtype;              /* cmoe_dtype of residual, residual_out, weight, h */
+    int32_t delta_dtype;        /* cmoe_dtype of delta                             */
+    float eps;                  /* finite, >= 0                                    */
+    const void* residual;
+    int64_t residual_stride;
+    const void* delta;          /* NULL: nothing is added                          */
+    int64_t delta_stride;
+    void* residual_out;         /* r, or NULL                                      */
+    int64_t residual_out_stride;
+    const void* weight;         /* [d], or NULL: ones                              */
+    void* h;                    /* or NULL                                         */
+    int64_t h_stride;
+    uint8_t* h8;                /* or NULL; needs d % 32 == 0                      */
+    int64_t h8_stride;
+    uint8_t* h8_scale;          /* [rows] rows of d / 32; with h8                  */
+    int64_t h8_scale_stride;
+    const int32_t* n_rows;      /* device: rows behind *n_rows (held to [0, rows])
+                                   are neither read nor written; NULL: all rows    */
+} cmoe_norm;
+
+cmoe_status cmoe_add_norm(const cmoe_norm* n, void* stream);
+
+/* Rows of fp32 or bf16 values (src, dtype) into 8 bits: q takes a byte a value,
+ * scale one for every 32.  cols a multiple of 32; rows of src and q 16-byte
+ * aligned; strides as in cmoe_norm.  Expert pools go in whole, with the last
+ * dimension of each matrix (d, d, F) a multiple of 32: rows = 1, cols = 3 d F. */
+cmoe_status cmoe_quantize(const void* src, int32_t dtype, int64_t rows, int64_t cols, int64_t src_stride,
+                          uint8_t* q, int64_t q_stride, uint8_t* scale, int64_t scale_stride, void* stream);
+
+/* How weights or activations of the layer are held. */
+typedef enum {
+    CMOE_FORMAT_DTYPE = 0, /* in the configuration's dtype                        */
+    CMOE_FORMAT_MX8 = 1    /* in 8 bits with scales (dtype CMOE_BF16)             */
+} cmoe_format;
+
+/* Shape of L MoE layers run without caches.  1 <= K <= N.  Supported: N <= 256,
+ * K <= 64, d and F multiples of 64 up to 65536, T <= 64 (cmoe_step takes larger
+ * batches).  8-bit activations go with 8-bit weights. */
+typedef struct {
+    int32_t L, N, K, d, F;
+    int32_t T;           /* tokens of a call, at most                             */
+    int32_t dtype;       /* cmoe_dtype of the router and the hidden states        */
+    int32_t weights;     /* cmoe_format of the expert weights                     */
+    int32_t activations; /* cmoe_format of the experts' input                     */
+} cmoe_moe_config;
+
+/* Device pointers.  experts: the cold pool's layout, [L][N] x (W_gate[F][d],
+ * W_up[F][d], W_down[d][F]), in dtype or one byte a value with expert_scales
+ * [L][N][3 d F / 32]; the same pool can serve a cmoe_handle. */
+typedef struct {
+    const void* w_router;         /* [L][N][d]                                     */
+    const float* logit_bias;      /* [L][N] fp32 or NULL; -inf takes an expert out */
+    const void* experts;
+    const uint8_t* expert_scales; /* with CMOE_FORMAT_MX8, else ignored            */
+} cmoe_moe_weights;
+
+typedef struct cmoe_moe cmoe_moe;
+
+/* Workspace bytes of a configuration.  Pure host code. */
+cmoe_status cmoe_moe_query(const cmoe_moe_config* cfg, size_t* workspace_bytes);
+
+/* Binds weights, a workspace (256-byte aligned) and a stream.  The handle
+ * belongs to the device that is current during this call. */
+cmoe_status cmoe_moe_init(const cmoe_moe_config* cfg, const cmoe_moe_weights* w, void* workspace, void* stream,
+                          cmoe_moe** out);
+
+/* One layer's call.  Strides count values (h8 and h8_scale: bytes); rows of h
+ * and y are 16-byte aligned; outputs overlap no input and no other output. */
+typedef struct {
+    int32_t layer;
+    int32_t T;                /* rows, 0 .. the configuration's T                   */
+    const void* h;            /* hidden states in dtype: the router's input, and the
+                                 experts' unless the activations are 8-bit          */
+    int64_t h_stride;
+    const uint8_t* h8;        /* with 8-bit activations: the experts' input         */
+    int64_t h8_stride;
+    const uint8_t* h8_scale;
+    int64_t h8_scale_stride;
+    float* y;                 /* fp32 output rows                                   */
+    int64_t y_stride;
+    const int32_t* n_tokens;  /* device: rows behind *n_tokens (held to [0, T]) are
+                                 padding, not read and left as they were in every
+                                 output; NULL: all rows are tokens                  */
+    int32_t* selected;        /* [T][K] selected experts in descending logit, or NULL */
+    float* gates;             /* [T][K] their weights, or NULL                      */
+} cmoe_moe_call;
+
+/* One MoE layer for T tokens: the native router and Top-K (lower index on equal
+ * logits; fp64 sums, rounded to fp32 once with the bias), gates = softmax over
+ * the selected logits, and y = sum_k gate_k W_down,k (silu(W_gate,k x) *
+ * (W_up,k x)), k in descending logit, with fp32 sums and an intermediate that is
+ * not rounded to fewer bits.  Experts with a logit of -inf are not selected
+ * (index -1, gate 0); a token that selects none gets y = 0.  A NaN logit counts
+ * as the largest and makes the token's gates and y NaN. */
+cmoe_status cmoe_moe_layer(cmoe_moe* hd, const cmoe_moe_call* c);
+
+/* cmoe_add_norm followed by the layer: h is the norm's output (and, with 8-bit
+ * activations, its 8-bit output), held in the workspace.  n: rows = c->T, d and
+ * dtype of the configuration; h, h8, h8_scale and n_rows NULL (c->n_tokens counts
+ * for both).  c: h, h8 and h8_scale NULL. */
+cmoe_status cmoe_moe_block(cmoe_moe* hd, const cmoe_norm* n, const cmoe_moe_call* c);
+
+/* Releases the handle (not the caller's buffers).  NULL is accepted. */
+cmoe_status cmoe_moe_destroy(cmoe_moe* hd);
+
 const char* cmoe_last_error(void);
 
 #ifdef __cplusplus

@@ -5,4 +5,4 @@ Importing the package does not load the library; ``cmoe.lib()`` does, and
 raises if libcmoe.so has not been built.  There is no CPU fallback.
 """
 from . import cmoe  # noqa: F401
-from .cmoe import CmoeError, Engine, cmoe_query, lib, make_config  # noqa: F401
+from .cmoe import CmoeError, Engine, MoeLayers, cmoe_query, lib, make_config, make_moe_config  # noqa: F401

@@ -38,6 +38,9 @@ CMOE_FLAG_FFN_GROUPED = 0x2
 CMOE_FLAG_FFN_SINGLE = 0x4
 CMOE_FLAG_FILL_ON_SIDE = 0x8
 
+CMOE_FORMAT_DTYPE = 0
+CMOE_FORMAT_MX8 = 1
+
 CMOE_VIEW_LOGITS = 0
 CMOE_VIEW_SELECTED = 1
 CMOE_VIEW_GATES = 2
@@ -55,7 +58,8 @@ KERNEL_NAMES = ("router", "cache_step", "fill", "ffn_up", "ffn_down", "combine")
 
 EXPORTED = ("cmoe_query", "cmoe_init", "cmoe_step", "cmoe_step_noalloc", "cmoe_step_logits", "cmoe_stats", "cmoe_get_cache",
             "cmoe_set_cache", "cmoe_set_R", "cmoe_reset", "cmoe_destroy", "cmoe_view_bytes", "cmoe_read",
-            "cmoe_profile_begin", "cmoe_profile_end", "cmoe_concentration", "cmoe_read_probe", "cmoe_last_error")
+            "cmoe_profile_begin", "cmoe_profile_end", "cmoe_concentration", "cmoe_read_probe", "cmoe_add_norm", "cmoe_quantize",
+            "cmoe_moe_query", "cmoe_moe_init", "cmoe_moe_layer", "cmoe_moe_block", "cmoe_moe_destroy", "cmoe_last_error")
 
 
 class cmoe_config(ctypes.Structure):
@@ -85,6 +89,28 @@ class cmoe_stats_t(ctypes.Structure):
 
     def as_dict(self):
         return {n: int(getattr(self, n)) for n, _ in self._fields_}
+
+
+class cmoe_norm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "d", "dtype", "delta_dtype")] + [("eps", ctypes.c_float)] + \
+        [f for n in ("residual", "delta", "residual_out") for f in ((n, ctypes.c_void_p), (n + "_stride", ctypes.c_int64))] + \
+        [("weight", ctypes.c_void_p)] + \
+        [f for n in ("h", "h8", "h8_scale") for f in ((n, ctypes.c_void_p), (n + "_stride", ctypes.c_int64))] + \
+        [("n_rows", ctypes.c_void_p)]
+
+
+class cmoe_moe_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("L", "N", "K", "d", "F", "T", "dtype", "weights", "activations")]
+
+
+class cmoe_moe_weights(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w_router", "logit_bias", "experts", "expert_scales")]
+
+
+class cmoe_moe_call(ctypes.Structure):
+    _fields_ = [("layer", ctypes.c_int32), ("T", ctypes.c_int32)] + \
+        [f for n in ("h", "h8", "h8_scale", "y") for f in ((n, ctypes.c_void_p), (n + "_stride", ctypes.c_int64))] + \
+        [(n, ctypes.c_void_p) for n in ("n_tokens", "selected", "gates")]
 
 
 class CmoeError(RuntimeError):
@@ -123,6 +149,14 @@ def lib():
         L.cmoe_profile_end.argtypes = [vp, ctypes.POINTER(ctypes.c_double), i64p]
         L.cmoe_concentration.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double)]
         L.cmoe_read_probe.argtypes = [vp, ctypes.c_int64, i32, ctypes.POINTER(ctypes.c_double)]
+        i64, ref = ctypes.c_int64, ctypes.POINTER
+        L.cmoe_add_norm.argtypes = [ref(cmoe_norm), vp]
+        L.cmoe_quantize.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp]
+        L.cmoe_moe_query.argtypes = [ref(cmoe_moe_config), ref(ctypes.c_size_t)]
+        L.cmoe_moe_init.argtypes = [ref(cmoe_moe_config), ref(cmoe_moe_weights), vp, vp, ref(vp)]
+        L.cmoe_moe_layer.argtypes = [vp, ref(cmoe_moe_call)]
+        L.cmoe_moe_block.argtypes = [vp, ref(cmoe_norm), ref(cmoe_moe_call)]
+        L.cmoe_moe_destroy.argtypes = [vp]
         L.cmoe_last_error.argtypes = []
         L.cmoe_last_error.restype = ctypes.c_char_p
         for n in EXPORTED:
@@ -298,5 +332,202 @@ class Engine:
     def __del__(self):
         try:
             self.cmoe_destroy()
+        except Exception:
+            pass
+
+
+# ------------------------------------------------------------ operators without a cache
+def _invalid(msg):
+    raise CmoeError(CMOE_ERR_INVALID_ARG, msg)
+
+
+def _rows(t, name, dtype, rows, cols, device):
+    """Address and row stride of a device tensor [rows][cols] whose rows are
+    contiguous; raises on any other tensor."""
+    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.device != device:
+        _invalid(f"{name} must be a [{rows}][{cols}] tensor of {dtype} on {device}")
+    if cols > 1 and t.stride(1) != 1:
+        _invalid(f"the rows of {name} must be contiguous")
+    return t.data_ptr(), (t.stride(0) if rows > 1 else cols)
+
+
+def _flat(t, name, dtype, numel, device):
+    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous() or t.device != device:
+        _invalid(f"{name} must be a contiguous tensor of {numel} values of {dtype} on {device}")
+    return t.data_ptr()
+
+
+def _types():
+    import torch
+    return {torch.float32: CMOE_F32, torch.bfloat16: CMOE_BF16}
+
+
+def _stream_of(torch, stream, device):
+    """hipStream_t of `stream`, or of the current stream; the work goes to the
+    current device, so the tensors have to be there."""
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        _invalid("the tensors must be on the current device")
+    return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+
+
+def _norm_args(residual, delta, weight, eps, residual_out, h, h8, h8_scale, n_rows):
+    import torch
+    if residual.dim() != 2 or residual.dtype not in _types():
+        _invalid("residual must be a [rows][d] tensor of float32 or bfloat16")
+    (rows, d), dt, dev = residual.shape, residual.dtype, residual.device
+    a = cmoe_norm(rows=rows, d=d, dtype=_types()[dt], eps=eps)
+    a.residual, a.residual_stride = _rows(residual, "residual", dt, rows, d, dev)
+    if delta is not None:
+        if delta.dtype not in _types():
+            _invalid("delta must be float32 or bfloat16")
+        a.delta_dtype = _types()[delta.dtype]
+        a.delta, a.delta_stride = _rows(delta, "delta", delta.dtype, rows, d, dev)
+    if weight is not None:
+        a.weight = _flat(weight, "weight", dt, d, dev)
+    if residual_out is not None:
+        a.residual_out, a.residual_out_stride = _rows(residual_out, "residual_out", dt, rows, d, dev)
+    if h is not None:
+        a.h, a.h_stride = _rows(h, "h", dt, rows, d, dev)
+    if h8 is not None:
+        a.h8, a.h8_stride = _rows(h8, "h8", torch.uint8, rows, d, dev)
+    if h8_scale is not None:
+        a.h8_scale, a.h8_scale_stride = _rows(h8_scale, "h8_scale", torch.uint8, rows, d // 32, dev)
+    if n_rows is not None:
+        a.n_rows = _flat(n_rows, "n_rows", torch.int32, 1, dev)
+    return a
+
+
+def cmoe_add_norm(residual, delta=None, weight=None, eps=1e-6, residual_out=None, h=None, h8=None, h8_scale=None,
+                  n_rows=None, stream=None):
+    """The residual's addition and RMS norm (see the header) of [rows][d]
+    tensors into the outputs given, on `stream` or the current one.  residual_out
+    may be residual."""
+    import torch
+    a = _norm_args(residual, delta, weight, eps, residual_out, h, h8, h8_scale, n_rows)
+    _check(lib().cmoe_add_norm(a, _stream_of(torch, stream, residual.device)))
+
+
+def cmoe_quantize(src, q, scale, stream=None):
+    """[rows][cols] values of float32 or bfloat16 into 8 bits: q [rows][cols]
+    and scale [rows][cols / 32], both uint8."""
+    import torch
+    if src.dim() != 2 or src.dtype not in _types():
+        _invalid("src must be a [rows][cols] tensor of float32 or bfloat16")
+    rows, cols = src.shape
+    p, stride = _rows(src, "src", src.dtype, rows, cols, src.device)
+    pq, q_stride = _rows(q, "q", torch.uint8, rows, cols, src.device)
+    ps, s_stride = _rows(scale, "scale", torch.uint8, rows, cols // 32, src.device)
+    _check(lib().cmoe_quantize(p, _types()[src.dtype], rows, cols, stride, pq, q_stride, ps, s_stride,
+                               _stream_of(torch, stream, src.device)))
+
+
+def quantize_experts(experts):
+    """A pool [L][N][3 d F] in 8 bits: (values, scales) [L][N][3 d F] and
+    [L][N][3 d F / 32], for MoeLayers with CMOE_FORMAT_MX8."""
+    import torch
+    if not experts.is_contiguous() or experts.dim() != 3:
+        _invalid("experts must be a contiguous [L][N][3 d F] tensor")
+    L, N, n = experts.shape
+    q = torch.empty((L, N, n), dtype=torch.uint8, device=experts.device)
+    scale = torch.empty((L, N, n // 32), dtype=torch.uint8, device=experts.device)
+    cmoe_quantize(experts.view(L * N, n), q.view(L * N, n), scale.view(L * N, n // 32))
+    return q, scale
+
+
+def make_moe_config(L, N, K, d, F, T, dtype, weights=CMOE_FORMAT_DTYPE, activations=CMOE_FORMAT_DTYPE):
+    return cmoe_moe_config(L, N, K, d, F, T, dtype, weights, activations)
+
+
+def cmoe_moe_query(cfg: cmoe_moe_config) -> int:
+    out = ctypes.c_size_t()
+    _check(lib().cmoe_moe_query(ctypes.byref(cfg), ctypes.byref(out)))
+    return out.value
+
+
+class MoeLayers:
+    """L MoE layers without caches: one handle plus its workspace.  The weights
+    are the caller's tensors: w_router [L][N][d], logit_bias [L][N] fp32 or
+    None, experts [L][N][3 d F] (expert_scales [L][N][3 d F / 32] with 8-bit
+    ones), norm_weight [L][d] or None (ones) for cmoe_moe_block.  All calls run
+    on `stream` (default: the stream that is current here)."""
+
+    def __init__(self, cfg: cmoe_moe_config, w_router, logit_bias, experts, expert_scales=None, norm_weight=None,
+                 norm_eps=1e-6, stream=None):
+        import torch
+        self.handle = None
+        self.cfg = cfg
+        size = cmoe_moe_query(cfg)
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.dtype = torch.bfloat16 if cfg.dtype == CMOE_BF16 else torch.float32
+        n = cfg.L * cfg.N * 3 * cfg.d * cfg.F
+        mx8 = cfg.weights == CMOE_FORMAT_MX8
+        w = cmoe_moe_weights(
+            _flat(w_router, "w_router", self.dtype, cfg.L * cfg.N * cfg.d, self.device),
+            None if logit_bias is None else _flat(logit_bias, "logit_bias", torch.float32, cfg.L * cfg.N, self.device),
+            _flat(experts, "experts", torch.uint8 if mx8 else self.dtype, n, self.device), None)
+        if mx8:
+            if expert_scales is None:
+                _invalid("8-bit experts need expert_scales")
+            w.expert_scales = _flat(expert_scales, "expert_scales", torch.uint8, n // 32, self.device)
+        if norm_weight is not None:
+            _flat(norm_weight, "norm_weight", self.dtype, cfg.L * cfg.d, self.device)
+            norm_weight = norm_weight.view(cfg.L, cfg.d)
+        self.norm_weight, self.norm_eps = norm_weight, norm_eps
+        self._keep = (w_router, logit_bias, experts, expert_scales)
+        self.stream = stream if stream is not None else torch.cuda.current_stream()
+        self.workspace = torch.empty(max(size, 256), dtype=torch.uint8, device=self.device)
+        self.workspace.record_stream(self.stream)
+        h = ctypes.c_void_p()
+        _check(lib().cmoe_moe_init(ctypes.byref(cfg), ctypes.byref(w), self.workspace.data_ptr(),
+                                   ctypes.c_void_p(self.stream.cuda_stream), ctypes.byref(h)))
+        self.handle = h
+
+    def _call(self, layer, T, y, n_tokens, selected, gates):
+        import torch
+        cfg, dev = self.cfg, self.device
+        c = cmoe_moe_call(layer=layer, T=T)
+        c.y, c.y_stride = _rows(y, "y", torch.float32, T, cfg.d, dev)
+        if n_tokens is not None:
+            c.n_tokens = _flat(n_tokens, "n_tokens", torch.int32, 1, dev)
+        if selected is not None:
+            c.selected = _flat(selected, "selected", torch.int32, T * cfg.K, dev)
+        if gates is not None:
+            c.gates = _flat(gates, "gates", torch.float32, T * cfg.K, dev)
+        return c
+
+    def cmoe_moe_layer(self, layer, h, y, h8=None, h8_scale=None, n_tokens=None, selected=None, gates=None):
+        """y [T][d] = the layer's output for the hidden states h [T][d]; the
+        rows of both may be apart.  h8 and h8_scale: the experts' input with
+        8-bit activations.  selected, gates: [T][K]."""
+        import torch
+        d, T = self.cfg.d, h.shape[0]
+        c = self._call(layer, T, y, n_tokens, selected, gates)
+        c.h, c.h_stride = _rows(h, "h", self.dtype, T, d, self.device)
+        if h8 is not None:
+            c.h8, c.h8_stride = _rows(h8, "h8", torch.uint8, T, d, self.device)
+        if h8_scale is not None:
+            c.h8_scale, c.h8_scale_stride = _rows(h8_scale, "h8_scale", torch.uint8, T, d // 32, self.device)
+        _check(lib().cmoe_moe_layer(self.handle, c))
+
+    def cmoe_moe_block(self, layer, residual, delta, y, residual_out=None, n_tokens=None, selected=None, gates=None):
+        """Norm of residual + delta (None: of the residual), then the layer."""
+        cfg = self.cfg
+        if not 0 <= layer < cfg.L:
+            _invalid("layer must be in [0, L)")
+        w = None if self.norm_weight is None else self.norm_weight[layer]
+        n = _norm_args(residual, delta, w, self.norm_eps, residual_out, None, None, None, None)
+        if residual.device != self.device:
+            _invalid(f"residual must be on {self.device}")
+        c = self._call(layer, residual.shape[0], y, n_tokens, selected, gates)
+        _check(lib().cmoe_moe_block(self.handle, n, c))
+
+    def cmoe_moe_destroy(self):
+        if self.handle is not None:
+            _check(lib().cmoe_moe_destroy(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.cmoe_moe_destroy()
         except Exception:
             pass

@@ -73,6 +73,19 @@ cmoe_status fail(cmoe_status st, const std::string& msg) {
     return st;
 }
 
+}  // namespace
+
+int cmoe::set_error(int status, const char* msg) noexcept {
+    try {
+        g_err = msg;
+    } catch (...) {  // no memory for the text: the status alone
+        g_err.clear();
+    }
+    return status;
+}
+
+namespace {
+
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 enum KernelId { KID_ROUTER = 0, KID_CACHE = 1, KID_FILL = 2, KID_UP = 3, KID_DOWN = 4, KID_COMBINE = 5 };

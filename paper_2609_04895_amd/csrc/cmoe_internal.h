@@ -167,4 +167,78 @@ hipError_t launch_combine(const Layout& lo, int l0, int nl, float* y, hipStream_
 int64_t read_probe_bytes(int64_t bytes);
 hipError_t launch_read_probe(const void* src, int64_t bytes, hipStream_t st, const Timing& tm);
 
+// ------------------------------------------------ operators without a cache
+
+// Residual addition and norm of `rows` rows (strides in values, the 8-bit ones
+// in bytes; NULL: no such input or output).
+struct NormArgs {
+    int32_t rows, d, bf16, delta_bf16;
+    float eps;
+    const void* residual;
+    int64_t residual_stride;
+    const void* delta;
+    int64_t delta_stride;
+    void* residual_out;
+    int64_t residual_out_stride;
+    const void* weight;
+    void* h;
+    int64_t h_stride;
+    uint8_t* h8;
+    int64_t h8_stride;
+    uint8_t* h8_scale;
+    int64_t h8_scale_stride;
+    const int32_t* n_rows;  // rows behind *n_rows are not read and not written
+};
+// aligned: d % 8 == 0 and every row 16-byte aligned (8-bit rows: 8)
+hipError_t launch_norm(const NormArgs& a, bool aligned, hipStream_t st);
+
+struct QuantizeArgs {
+    int32_t bf16;
+    const void* src;
+    int64_t rows, cols, src_stride;
+    uint8_t* q;
+    int64_t q_stride;
+    uint8_t* scale;
+    int64_t scale_stride;
+};
+hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t st);
+
+constexpr int kMoeTokens = 64;      // tokens of a whole-layer call, at most: one bit each of a 64-bit mask
+constexpr int kMoeUnitTokens = 16;  // tokens of an expert in one pass over its weights: columns of a matrix-core tile
+enum MoeFormat { kMoeF32 = 0, kMoeBf16 = 1, kMoeMx8 = 2 };  // of the expert weights
+
+// One whole-layer call.
+struct MoeArgs {
+    int32_t N, K, d, F, T;
+    int32_t bf16;           // type of h and of the router
+    int32_t format;         // MoeFormat
+    const void* w_router;   // [N][d]
+    const float* bias;      // [N] or NULL
+    const void* experts;    // [N][3 d F]
+    const uint8_t* scales;  // [N][3 d F / 32], kMoeMx8
+    const void* h;          // [T] rows
+    int64_t h_stride;
+    const uint8_t* h8;      // [T] rows of 8-bit values, the experts' input instead of h, or NULL
+    int64_t h8_stride;
+    const uint8_t* h8_scale;
+    int64_t h8_scale_stride;
+    float* y;               // [T] rows
+    int64_t y_stride;
+    const int32_t* n_tokens;
+    int32_t* selected;      // [T][K] or NULL
+    float* gates;           // [T][K] or NULL
+    // workspace
+    float* z;               // [T][N]   logits
+    int32_t* sel;           // [T][K]   selected experts, -1: none
+    float* gate;            // [T][K]
+    uint16_t* x;            // [T][d]   bf16 values of h8
+    void* act;              // SwiGLU intermediate by row: [3][F] bf16 or [F] fp32
+    float* out;             // [rows][d] expert outputs; a row is one (expert, token), in that order
+};
+hipError_t launch_moe(const MoeArgs& a, hipStream_t st);
+
+// Sets the calling thread's error text and returns the status, for entry points
+// outside cmoe.cpp.
+int set_error(int status, const char* msg) noexcept;
+
 }  // namespace cmoe

@@ -1,0 +1,320 @@
+// norm.hip - what stands between two layer steps: the residual's addition with
+// its root-mean-square norm, r = fl(residual + delta), h = r w / sqrt(mean r^2 +
+// eps), and rows into 8 bits (mx8.h), as an output of the norm or on their own.
+//
+// One pass over the data: each thread keeps its values of a row in registers
+// between the sum of squares and the outputs, so every input is read and every
+// output written once.  Both kernels are bound by HBM for many rows and by the
+// launch and one trip to memory for few.
+//
+// r is rounded to the residual's type before it is squared, so that the norm is
+// that of the residual as stored.  Sums are fp32.  The 8-bit output is rounded
+// from the fp32 value of h, not from its bf16 form: one rounding.
+#include "cmoe_internal.h"
+#include "mx8.h"
+
+namespace cmoe {
+
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+// Eight consecutive values, widened to fp32.
+template <bool BF16>
+__device__ inline void load8(const void* p, int64_t i, float* v) {
+    if constexpr (BF16) {
+        const bf16x8 r = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(p) + i);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = (float)r[j];
+    } else {
+        const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
+        const f32x4 a = q[0], b = q[1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            v[j] = a[j];
+            v[4 + j] = b[j];
+        }
+    }
+}
+
+template <bool BF16>
+__device__ inline void store8(void* p, int64_t i, const float* v) {
+    if constexpr (BF16) {
+        bf16x8 r;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r[j] = (__bf16)v[j];
+        *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p) + i) = r;
+    } else {
+        f32x4* q = reinterpret_cast<f32x4*>(static_cast<float*>(p) + i);
+        q[0] = f32x4{v[0], v[1], v[2], v[3]};
+        q[1] = f32x4{v[4], v[5], v[6], v[7]};
+    }
+}
+
+template <bool BF16>
+__device__ inline float load1(const void* p, int64_t i) {
+    if constexpr (BF16)
+        return (float)static_cast<const __bf16*>(p)[i];
+    else
+        return static_cast<const float*>(p)[i];
+}
+
+template <bool BF16>
+__device__ inline float rounded(float v) {
+    if constexpr (BF16)
+        return (float)(__bf16)v;
+    else
+        return v;
+}
+
+template <bool BF16>
+__device__ inline void store1(void* p, int64_t i, float v) {
+    if constexpr (BF16)
+        static_cast<__bf16*>(p)[i] = (__bf16)v;
+    else
+        static_cast<float*>(p)[i] = v;
+}
+
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m);
+    return v;
+}
+
+// Sum over the TPR threads of a row, in a fixed order; every thread gets it.
+// TPR > 64: red holds one partial per wavefront and the row is the workgroup's.
+template <int TPR>
+__device__ inline float row_sum(float v, float* red) {
+    v = wave_sum(v);
+    if constexpr (TPR > 64) {
+        const int wv = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) red[wv] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < TPR / 64; ++w) v += red[w];
+    }
+    return v;
+}
+
+__device__ inline int live_rows(const NormArgs& a) {
+    return a.n_rows ? min(max(*a.n_rows, 0), a.rows) : a.rows;
+}
+
+constexpr int kThreads = 256;  // threads of a workgroup with one wavefront per row: four rows
+
+// d % 8 == 0 and every row 16-byte aligned.  TPR threads per row, thread t taking
+// the groups of 8 values t, t + TPR, ... (NV at most); the four groups of a block
+// of 32 lie in neighbouring lanes.
+template <bool BF16, int DELTA, int TPR, int NV>
+__global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(NormArgs a) {
+    __shared__ float red[TPR > 64 ? TPR / 64 : 1];
+    constexpr int RPG = TPR >= kThreads ? 1 : kThreads / TPR;  // rows per workgroup
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * RPG + threadIdx.x / TPR;
+    if (row >= live_rows(a)) return;  // whole wavefronts, and whole workgroups where they share a row
+    const int ng = a.d / 8;
+    float r[NV][8] = {};
+    float ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int g = t + i * TPR;
+        if (g < ng) load8<BF16>(a.residual, row * a.residual_stride + 8 * g, r[i]);
+    }
+    if constexpr (DELTA != 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int g = t + i * TPR;
+            if (g < ng) {
+                float v[8];
+                load8<DELTA == 2>(a.delta, row * a.delta_stride + 8 * g, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) r[i][j] = rounded<BF16>(r[i][j] + v[j]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int g = t + i * TPR;
+        if (g < ng) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) ss += r[i][j] * r[i][j];
+            if (a.residual_out) store8<BF16>(a.residual_out, row * a.residual_out_stride + 8 * g, r[i]);
+        }
+    }
+    const float s = 1.0f / sqrtf(row_sum<TPR>(ss, red) / (float)a.d + a.eps);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int g = t + i * TPR;
+        const bool in = g < ng;
+        if (in) {
+            float w[8];
+            if (a.weight) load8<BF16>(a.weight, 8 * g, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r[i][j] = a.weight ? r[i][j] * s * w[j] : r[i][j] * s;
+            if (a.h) store8<BF16>(a.h, row * a.h_stride + 8 * g, r[i]);
+        }
+        if (a.h8) {  // d % 32 == 0: the lanes of a block are all in or all out
+            float m = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = mx_max(m, r[i][j]);
+            m = mx_max(m, __shfl_xor(m, 1));
+            m = mx_max(m, __shfl_xor(m, 2));
+            if (in) {
+                const uint32_t byte = mx_scale_byte(m);
+                *reinterpret_cast<uint2*>(a.h8 + row * a.h8_stride + 8 * g) = mx_pack8(r[i], byte);
+                if ((g & 3) == 0) a.h8_scale[row * a.h8_scale_stride + g / 4] = (uint8_t)byte;
+            }
+        }
+    }
+}
+
+// Any d, any alignment: one workgroup per row, one value per thread and step.
+// The second pass reads the inputs again (from the caches) and does the
+// additions again.
+template <bool BF16, int DELTA>
+__global__ __launch_bounds__(kThreads) void norm_any_kernel(NormArgs a) {
+    __shared__ float red[kThreads / 64];
+    const int64_t row = blockIdx.x;
+    if (row >= live_rows(a)) return;
+    auto value = [&](int i) {
+        float v = load1<BF16>(a.residual, row * a.residual_stride + i);
+        if constexpr (DELTA != 0) v = rounded<BF16>(v + load1<DELTA == 2>(a.delta, row * a.delta_stride + i));
+        return v;
+    };
+    float ss = 0.0f;
+    for (int i = threadIdx.x; i < a.d; i += kThreads) {
+        const float v = value(i);
+        ss += v * v;
+    }
+    const float s = 1.0f / sqrtf(row_sum<kThreads>(ss, red) / (float)a.d + a.eps);
+    for (int i0 = 0; i0 < a.d; i0 += kThreads) {
+        const int i = i0 + threadIdx.x;
+        float v = 0.0f;
+        if (i < a.d) {
+            v = value(i);
+            // every element is read for the last time by the thread that overwrites it
+            if (a.residual_out) store1<BF16>(a.residual_out, row * a.residual_out_stride + i, v);
+            v *= s;
+            if (a.weight) v *= load1<BF16>(a.weight, i);
+            if (a.h) store1<BF16>(a.h, row * a.h_stride + i, v);
+        }
+        if (a.h8) {
+            float m = mx_max(v, 0.0f);
+#pragma unroll
+            for (int k = 1; k < kMxBlock; k <<= 1) m = mx_max(m, __shfl_xor(m, k));
+            if (i < a.d) {
+                const uint32_t byte = mx_scale_byte(m);
+                a.h8[row * a.h8_stride + i] =
+                    (uint8_t)(byte == kMxBad ? kMxNaN2 : mx_pair<false>(v, v, mx_inverse(byte), 0));
+                if (i % kMxBlock == 0) a.h8_scale[row * a.h8_scale_stride + i / kMxBlock] = (uint8_t)byte;
+            }
+        }
+    }
+}
+
+template <bool BF16, int DELTA>
+hipError_t launch_norm_t(const NormArgs& a, bool aligned, hipStream_t st) {
+    const int ng = a.d / 8;
+    auto go = [&](auto kernel, int tpr) {
+        const int rpg = tpr >= kThreads ? 1 : kThreads / tpr;
+        launch_kernel(kernel, dim3((unsigned)((a.rows + rpg - 1) / rpg)), dim3(tpr > kThreads ? tpr : kThreads), st, Timing{}, a);
+    };
+    if (!aligned || ng > 4096)
+        go(norm_any_kernel<BF16, DELTA>, kThreads);
+    else if (a.rows >= 1024 && ng <= 512) {
+        if (ng <= 64)
+            go(norm_kernel<BF16, DELTA, 64, 1>, 64);
+        else if (ng <= 128)
+            go(norm_kernel<BF16, DELTA, 64, 2>, 64);
+        else if (ng <= 256)
+            go(norm_kernel<BF16, DELTA, 64, 4>, 64);
+        else
+            go(norm_kernel<BF16, DELTA, 64, 8>, 64);
+    } else if (ng <= 256)
+        go(norm_kernel<BF16, DELTA, 256, 1>, 256);
+    else if (ng <= 512)
+        go(norm_kernel<BF16, DELTA, 256, 2>, 256);
+    else if (ng <= 1024)
+        go(norm_kernel<BF16, DELTA, 1024, 1>, 1024);
+    else
+        go(norm_kernel<BF16, DELTA, 1024, 4>, 1024);
+    return hipGetLastError();
+}
+
+// Sixteen values per thread, half a block, 16-byte loads and stores.  unit: the
+// half block's number in its row.
+template <bool BF16>
+__device__ inline void quantize16(const void* src, int64_t at, uint8_t* q, uint8_t* scale, int64_t unit, bool in) {
+    float v[16] = {};
+    float m = 0.0f;
+    if (in) {
+        load8<BF16>(src, at, v);
+        load8<BF16>(src, at + 8, v + 8);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) m = mx_max(m, v[j]);
+    }
+    m = mx_max(m, __shfl_xor(m, 1));
+    if (!in) return;
+    const uint32_t byte = mx_scale_byte(m);
+    const uint2 a = mx_pack8(v, byte), b = mx_pack8(v + 8, byte);
+    *reinterpret_cast<u32x4*>(q + 16 * unit) = u32x4{a.x, a.y, b.x, b.y};
+    if ((unit & 1) == 0) scale[unit / 2] = (uint8_t)byte;
+}
+
+// Rows that follow each other without gaps: one long row.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void quantize_flat_kernel(QuantizeArgs a) {
+    const int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const bool in = u < a.rows * (a.cols / 16);
+    quantize16<BF16>(a.src, 16 * u, a.q, a.scale, u, in);
+}
+
+// Rows apart: tpr threads (a power of two, at least 2) per row and step.
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void quantize_rows_kernel(QuantizeArgs a, int tpr) {
+    const int64_t row = (int64_t)blockIdx.x * (kThreads / tpr) + threadIdx.x / tpr;
+    const int t = threadIdx.x % tpr, n = (int)(a.cols / 16);
+    for (int u0 = 0; u0 < n; u0 += tpr) {
+        const int u = u0 + t;
+        quantize16<BF16>(a.src, row * a.src_stride + (int64_t)16 * u, a.q + row * a.q_stride, a.scale + row * a.scale_stride, u,
+                         row < a.rows && u < n);
+    }
+}
+
+template <bool BF16>
+hipError_t launch_quantize_t(const QuantizeArgs& a, hipStream_t st) {
+    const int64_t units = a.rows * (a.cols / 16);
+    if (a.src_stride == a.cols && a.q_stride == a.cols && a.scale_stride == a.cols / kMxBlock) {
+        launch_kernel(quantize_flat_kernel<BF16>, dim3((unsigned)((units + kThreads - 1) / kThreads)), dim3(kThreads), st,
+                      Timing{}, a);
+    } else {
+        int tpr = 2;
+        while (tpr < kThreads && tpr < a.cols / 16) tpr *= 2;
+        const int64_t rpg = kThreads / tpr;
+        launch_kernel(quantize_rows_kernel<BF16>, dim3((unsigned)((a.rows + rpg - 1) / rpg)), dim3(kThreads), st, Timing{}, a,
+                      tpr);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_norm(const NormArgs& a, bool aligned, hipStream_t st) {
+    const int delta = a.delta == nullptr ? 0 : a.delta_bf16 ? 2 : 1;
+    if (a.bf16)
+        return delta == 0   ? launch_norm_t<true, 0>(a, aligned, st)
+               : delta == 1 ? launch_norm_t<true, 1>(a, aligned, st)
+                            : launch_norm_t<true, 2>(a, aligned, st);
+    return delta == 0   ? launch_norm_t<false, 0>(a, aligned, st)
+           : delta == 1 ? launch_norm_t<false, 1>(a, aligned, st)
+                        : launch_norm_t<false, 2>(a, aligned, st);
+}
+
+hipError_t launch_quantize(const QuantizeArgs& a, hipStream_t st) {
+    return a.bf16 ? launch_quantize_t<true>(a, st) : launch_quantize_t<false>(a, st);
+}
+
+}  // namespace cmoe

@@ -1,0 +1,300 @@
+"""cmoe_add_norm and cmoe_quantize against fp64 forms: every kernel variant,
+types, one row to many, odd widths, strides, missing inputs and outputs, zero,
+tiny, huge and non-finite values, rows behind the last, in place, graphs and
+other streams.
+
+Tolerances: h is off by norm_error(d) before its rounding and half a step of its
+type after it; an 8-bit value by half an e4m3 step (2^-4 of the value, 2^-10 of
+the scale below e4m3's normal range) of the fp32 h it is rounded from; r is exact."""
+import math
+
+import numpy as np
+import pytest
+
+import operator_reference as ref
+from gpu_util import say, stable_seed
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+BF16, F32 = torch.bfloat16, torch.float32
+EPS = 1e-6
+
+
+def rows_tensor(rows, d, dtype, gen, scale=1.0, gap=0):
+    """[rows][d] values with `gap` unused values between rows."""
+    full = (torch.randn((rows, d + gap), generator=gen) * scale).to(dtype).cuda()
+    return full[:, :d]
+
+
+def check_h(h, h64, d, dtype):
+    tol = ref.norm_error(d) + ref.HALF[dtype] * (1 if dtype == BF16 else 0) + 1e-30
+    off = (h.double().cpu() - h64).abs()
+    bad = off > tol * (1 + 2.0 ** -7) * h64.abs() + 1e-44
+    assert not bad.any(), f"h off by {(off / h64.abs().clamp(min=1e-300)).max():.3g}, allowed {tol:.3g}"
+
+
+def check_8bit(q8, scale, h64, d):
+    q8, scale = q8.cpu().contiguous(), scale.cpu().contiguous()
+    _, E, byte = ref.quantize(h64)
+    # a block's scale may differ only where amax lies within the fp32 error of a border
+    amax = h64.reshape(h64.shape[0], d // 32, 32).abs().amax(-1)
+    rel = ref.norm_error(d)
+    _, E_lo, _ = ref.quantize(h64 * (1 - 2 * rel))
+    _, E_hi, _ = ref.quantize(h64 * (1 + 2 * rel))
+    got = scale.int() - 127
+    assert ((got >= E_lo) & (got <= E_hi)).all()
+    v = ref.dequantize(q8, scale)
+    s = ref.pow2(got).unsqueeze(-1).expand(*got.shape, 32).reshape(h64.shape)
+    tol = torch.maximum(h64.abs() * (2.0 ** -4 + 2 * rel), s * 2.0 ** -10 * (1 + 1e-6))
+    assert ((v - h64).abs() <= tol * (1 + 2 * rel)).all()
+    assert (amax >= 0).all()
+
+
+SHAPES = [(1, 32), (1, 64), (3, 96), (1, 2048), (5, 2048), (7, 2880), (2, 4096), (3, 8192), (1, 8224), (1, 32768), (1, 32800),
+          (1024, 64), (1025, 512), (1030, 1024), (1027, 2048), (1025, 2880), (1024, 4096), (2, 8)]
+
+
+@pytest.mark.parametrize("rows,d", SHAPES)
+@pytest.mark.parametrize("dtype,delta", [(BF16, F32), (BF16, BF16), (BF16, None), (F32, F32), (F32, BF16), (F32, None)],
+                         ids=["bf16+f32", "bf16+bf16", "bf16", "f32+f32", "f32+bf16", "f32"])
+def test_norm_matches_fp64(rows, d, dtype, delta):
+    from paper_2609_04895_amd import cmoe as B
+    say("norm", rows, d, dtype, delta)
+    g = torch.Generator().manual_seed(stable_seed(f"norm {rows} {d} {dtype} {delta}"))
+    res = rows_tensor(rows, d, dtype, g, 4.0)
+    dl = None if delta is None else rows_tensor(rows, d, delta, g)
+    w = (1 + 0.1 * torch.randn(d, generator=g)).to(dtype).cuda()
+    out, h = torch.empty_like(res), torch.empty_like(res)
+    q, s = (torch.empty((rows, d), dtype=torch.uint8, device="cuda"), torch.empty((rows, d // 32), dtype=torch.uint8, device="cuda")) \
+        if d % 32 == 0 else (None, None)
+    B.cmoe_add_norm(res, dl, w, EPS, residual_out=out, h=h, h8=q, h8_scale=s)
+    r, h64 = ref.norm(res.cpu(), None if dl is None else dl.cpu(), w.cpu(), EPS)
+    assert torch.equal(out.cpu(), r)
+    check_h(h, h64, d, dtype)
+    if q is not None:
+        check_8bit(q, s, h64, d)
+    # each output alone gives the same, and no weight is a weight of ones
+    h2, q2, s2 = torch.empty_like(h), None if q is None else torch.empty_like(q), None if q is None else torch.empty_like(s)
+    B.cmoe_add_norm(res, dl, w, EPS, h=h2)
+    assert torch.equal(h, h2)
+    if q is not None:
+        B.cmoe_add_norm(res, dl, w, EPS, h8=q2, h8_scale=s2)
+        assert torch.equal(q, q2) and torch.equal(s, s2)
+    B.cmoe_add_norm(res, dl, None, EPS, h=h2)
+    h3 = torch.empty_like(h)
+    B.cmoe_add_norm(res, dl, torch.ones_like(w), EPS, h=h3)
+    assert torch.equal(h2, h3)
+
+
+@pytest.mark.parametrize("rows,d,gap", [(3, 1, 0), (2, 31, 0), (5, 1001, 0), (4, 2047, 3), (3, 64, 1), (6, 2048, 5), (9, 2880, 8),
+                                        (1026, 100, 0), (1, 40001, 0)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_odd_widths_and_rows_apart(rows, d, gap, dtype):
+    from paper_2609_04895_amd import cmoe as B
+    say("norm odd", rows, d, gap, dtype)
+    g = torch.Generator().manual_seed(stable_seed(f"odd {rows} {d} {gap}"))
+    res, dl = rows_tensor(rows, d, dtype, g, 3.0, gap), rows_tensor(rows, d, F32, g, 1.0, 2 * gap)
+    w = (1 + 0.1 * torch.randn(d, generator=g)).to(dtype).cuda()
+    out = torch.full((rows, d + gap + 1), 7.0, dtype=dtype, device="cuda")
+    h = torch.full((rows, d + gap + 2), 7.0, dtype=dtype, device="cuda")
+    q = s = None
+    kw = {}
+    if d % 32 == 0:
+        q = torch.full((rows, d + 3 * gap), 9, dtype=torch.uint8, device="cuda")
+        s = torch.full((rows, d // 32 + gap), 9, dtype=torch.uint8, device="cuda")
+        kw = dict(h8=q[:, :d], h8_scale=s[:, :d // 32])
+    B.cmoe_add_norm(res, dl, w, EPS, residual_out=out[:, :d], h=h[:, :d], **kw)
+    r, h64 = ref.norm(res.cpu(), dl.cpu(), w.cpu(), EPS)
+    assert torch.equal(out[:, :d].cpu(), r)
+    check_h(h[:, :d], h64, d, dtype)
+    assert (out[:, d:] == 7).all() and (h[:, d:] == 7).all()  # nothing between the rows
+    if q is not None:
+        check_8bit(q[:, :d], s[:, :d // 32], h64, d)
+        assert (q[:, d:] == 9).all() and (s[:, d // 32:] == 9).all()
+
+
+@pytest.mark.parametrize("rows,d", [(1, 2048), (1100, 512), (3, 50)])
+def test_norm_in_place(rows, d):
+    from paper_2609_04895_amd import cmoe as B
+    g = torch.Generator().manual_seed(7)
+    res, dl = rows_tensor(rows, d, BF16, g, 4.0), rows_tensor(rows, d, F32, g)
+    a, ha, hb = torch.empty_like(res), torch.empty_like(res), torch.empty_like(res)
+    B.cmoe_add_norm(res, dl, None, EPS, residual_out=a, h=ha)
+    B.cmoe_add_norm(res, dl, None, EPS, residual_out=res, h=hb)
+    assert torch.equal(res, a) and torch.equal(ha, hb)
+
+
+@pytest.mark.parametrize("n", [-3, 0, 1, 5, 8, 9])
+@pytest.mark.parametrize("d", [64, 50])
+def test_rows_behind_the_last_are_left(n, d):
+    from paper_2609_04895_amd import cmoe as B
+    rows, live = 8, min(max(n, 0), 8)
+    g = torch.Generator().manual_seed(3)
+    res, dl = rows_tensor(rows, d, F32, g), rows_tensor(rows, d, F32, g)
+    res[live:] = math.nan
+    out, h = torch.full_like(res, 5.0), torch.full_like(res, 6.0)
+    q = torch.full((rows, d), 3, dtype=torch.uint8, device="cuda") if d % 32 == 0 else None
+    s = torch.full((rows, d // 32), 4, dtype=torch.uint8, device="cuda") if d % 32 == 0 else None
+    B.cmoe_add_norm(res, dl, None, EPS, residual_out=out, h=h, h8=q, h8_scale=s,
+                    n_rows=torch.tensor([n], dtype=torch.int32, device="cuda"))
+    r, h64 = ref.norm(res[:live].cpu(), dl[:live].cpu(), None, EPS)
+    assert torch.equal(out[:live].cpu(), r) and (out[live:] == 5).all() and (h[live:] == 6).all()
+    check_h(h[:live], h64, d, F32)
+    if q is not None:
+        assert (q[live:] == 3).all() and (s[live:] == 4).all()
+        check_8bit(q[:live], s[:live], h64, d)
+
+
+@pytest.mark.parametrize("d", [256, 50 * 32])
+def test_norm_rows_of_special_values(d):
+    """Zeros, values whose squares are below fp32's range, a NaN and an infinity:
+    each in its own row, the other rows unharmed."""
+    from paper_2609_04895_amd import cmoe as B
+    g = torch.Generator().manual_seed(5)
+    res = torch.randn((6, d), generator=g)
+    res[0] = 0.0
+    res[1] = 1e-30
+    res[2, 5] = math.nan
+    res[3, 40] = math.inf
+    res[4, :64] = 0.0
+    res = res.cuda()
+    h, q, s = torch.empty_like(res), torch.empty((6, d), dtype=torch.uint8, device="cuda"), \
+        torch.empty((6, d // 32), dtype=torch.uint8, device="cuda")
+    B.cmoe_add_norm(res, None, None, EPS, h=h, h8=q, h8_scale=s)
+    hc, v = h.cpu(), ref.dequantize(q.cpu(), s.cpu())
+    assert (hc[0] == 0).all() and (v[0] == 0).all() and (s[0] == 0).all()
+    assert torch.allclose(hc[1].double(), torch.full((d,), 1e-27, dtype=torch.float64), rtol=1e-5)
+    assert hc[2].isnan().all() and v[2].isnan().all() and (s[2] == 255).all()
+    # an infinity: mean and root are infinite, finite places become 0 and its own NaN
+    assert hc[3, 40].isnan() and (hc[3, :40] == 0).all() and (hc[3, 41:] == 0).all()
+    assert v[3, 32:64].isnan().all() and (v[3, :32] == 0).all() and (v[3, 64:] == 0).all()
+    for row in (4, 5):
+        _, h64 = ref.norm(res[row:row + 1].cpu(), None, None, EPS)
+        check_h(h[row:row + 1], h64, d, F32)
+        check_8bit(q[row:row + 1], s[row:row + 1], h64, d)
+
+
+def test_norm_offsets_past_32_bits():
+    """Two rows 2^31 + 64 values apart."""
+    from paper_2609_04895_amd import cmoe as B
+    d, apart = 256, (1 << 31) + 64
+    buf = torch.zeros(apart + d, dtype=BF16, device="cuda")
+    res = buf.as_strided((2, d), (apart, 1))
+    g = torch.Generator().manual_seed(11)
+    res[0], res[1] = torch.randn(d, generator=g).to(BF16).cuda(), torch.randn(d, generator=g).to(BF16).cuda()
+    keep = res.clone()
+    h = torch.empty((2, d), dtype=BF16, device="cuda")
+    B.cmoe_add_norm(res, None, None, EPS, residual_out=res, h=h)
+    _, h64 = ref.norm(keep.cpu(), None, None, EPS)
+    check_h(h, h64, d, BF16)
+    assert torch.equal(res, keep) and float(buf[d:d + 4096].abs().max()) == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols,gap", [(1, 32, 0), (1, 4096, 0), (3, 96, 0), (333, 4096, 0), (5, 64, 16), (17, 2080, 32), (2, 8192, 16)])
+def test_quantize_is_exact(rows, cols, gap, dtype):
+    """Bit for bit the definition, ties and borders among the values."""
+    from paper_2609_04895_amd import cmoe as B
+    say("quantize", rows, cols, gap, dtype)
+    g = torch.Generator().manual_seed(stable_seed(f"quantize {rows} {cols}"))
+    x = torch.randn((rows, cols + gap), generator=g) * torch.exp2(torch.randint(-40, 40, (rows, 1), generator=g).float())
+    # amax exactly on, just above and just below 448 2^k, values on e4m3 midpoints
+    x[0, :32] = torch.tensor([448.0, -447.0, 1.0625, 1.1875, 17.0, 19.0, 0.0] + [2.0 ** -k for k in range(25)])
+    if cols >= 96:
+        x[0, 32:64] = x[0, :32] * 2.0 ** -20
+        x[0, 32] = 448.0 * 2.0 ** -20 * (1 + 2.0 ** -7)
+        x[0, 64:96] = 0.0
+    x = x.to(dtype).cuda()[:, :cols]
+    q = torch.full((rows, cols + gap), 9, dtype=torch.uint8, device="cuda")
+    s = torch.full((rows, cols // 32 + gap), 9, dtype=torch.uint8, device="cuda")
+    B.cmoe_quantize(x, q[:, :cols], s[:, :cols // 32])
+    want, _, byte = ref.quantize(x.cpu())
+    assert torch.equal(s[:, :cols // 32].cpu().int(), byte.int())
+    got = q[:, :cols].cpu().contiguous().view(torch.float8_e4m3fn).double()
+    assert torch.equal(got, want)
+    assert (q[:, cols:] == 9).all() and (s[:, cols // 32:] == 9).all()
+
+
+def test_quantize_special_blocks():
+    """Non-finite blocks are NaN throughout, their neighbours unharmed; the
+    smallest and the largest fp32 values."""
+    from paper_2609_04895_amd import cmoe as B
+    x = torch.ones((1, 32 * 7))
+    x[0, 3] = math.nan
+    x[0, 32 + 31] = math.inf
+    x[0, 64 + 16] = -math.inf
+    x[0, 96:128] = torch.tensor(np.array([1], np.int32).view(np.float32)[0].item())  # 2^-149
+    x[0, 128:160] = torch.finfo(torch.float32).max
+    x[0, 192:224] = 2.0 ** -126
+    q, s = torch.empty((1, 224), dtype=torch.uint8, device="cuda"), torch.empty((1, 7), dtype=torch.uint8, device="cuda")
+    B.cmoe_quantize(x.cuda(), q, s)
+    want, _, byte = ref.quantize(x)
+    assert torch.equal(s.cpu().int(), byte.int()) and (byte[0, :3] == 255).all()
+    got = q.cpu().view(torch.float8_e4m3fn).double()
+    assert torch.equal(got.isnan(), want.isnan())
+    assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
+
+
+def test_quantize_past_32_bits():
+    """2^32 + 2^20 values in one call: the parts behind 2^31 and 2^32 are those of
+    a call on them alone."""
+    from paper_2609_04895_amd import cmoe as B
+    n = (1 << 32) + (1 << 20)
+    x = torch.empty((1, n), dtype=BF16, device="cuda")
+    x.view(-1, 1 << 20).copy_(torch.randn((1, 1 << 20), generator=torch.Generator().manual_seed(1)).cuda())
+    x.view(-1, 1 << 20).mul_(torch.arange(1, n // (1 << 20) + 1, device="cuda").to(BF16).unsqueeze(1))
+    q, s = torch.empty((1, n), dtype=torch.uint8, device="cuda"), torch.empty((1, n // 32), dtype=torch.uint8, device="cuda")
+    B.cmoe_quantize(x, q, s)
+    for at in (0, (1 << 31) - 4096, 1 << 31, (1 << 32) - 4096, n - 4096):
+        pq, ps = torch.empty((1, 4096), dtype=torch.uint8, device="cuda"), torch.empty((1, 128), dtype=torch.uint8, device="cuda")
+        B.cmoe_quantize(x[:, at:at + 4096].clone(), pq, ps)
+        assert torch.equal(q[:, at:at + 4096], pq) and torch.equal(s[:, at // 32:at // 32 + 128], ps), at
+
+
+def test_empty_calls_do_nothing():
+    from paper_2609_04895_amd import cmoe as B
+    e = torch.empty((0, 64), dtype=BF16, device="cuda")
+    B.cmoe_add_norm(e, None, None, EPS, h=torch.empty_like(e))
+    B.cmoe_quantize(e, torch.empty((0, 64), dtype=torch.uint8, device="cuda"), torch.empty((0, 2), dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+
+
+def test_norm_and_quantize_replayed_and_on_another_stream():
+    from paper_2609_04895_amd import cmoe as B
+    rows, d = 6, 2048
+    g = torch.Generator().manual_seed(9)
+    res, dl = rows_tensor(rows, d, BF16, g, 4.0), rows_tensor(rows, d, F32, g)
+    n = torch.tensor([rows], dtype=torch.int32, device="cuda")
+    out, h = torch.zeros_like(res), torch.zeros_like(res)
+    q, s = torch.zeros((rows, d), dtype=torch.uint8, device="cuda"), torch.zeros((rows, d // 32), dtype=torch.uint8, device="cuda")
+
+    def call():
+        B.cmoe_add_norm(res, dl, None, EPS, residual_out=out, h=h, n_rows=n)
+        B.cmoe_quantize(h, q, s)
+
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        call()
+    st.synchronize()
+    first = [t.clone() for t in (out, h, q, s)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        res.copy_(rows_tensor(rows, d, BF16, g, 1.0 + i))
+        n.fill_(rows - i)
+        for t in (out, h, q, s):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, h, q, s)]
+        for t in (out, h, q, s):
+            t.zero_()
+        call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (out, h, q, s))), i
+        assert (got[0][rows - i:] == 0).all()
+    assert not torch.equal(first[0], out)
