@@ -475,8 +475,8 @@ class MoeLayers:
         self.norm_weight, self.norm_eps = norm_weight, norm_eps
         self._keep = (w_router, logit_bias, experts, expert_scales)
         self.stream = stream if stream is not None else torch.cuda.current_stream()
-        self.workspace = torch.empty(max(size, 256), dtype=torch.uint8, device=self.device)
-        self.workspace.record_stream(self.stream)
+        with torch.cuda.stream(self.stream):  # the allocator's owner of the memory: the stream that uses it
+            self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
         h = ctypes.c_void_p()
         _check(lib().cmoe_moe_init(ctypes.byref(cfg), ctypes.byref(w), self.workspace.data_ptr(),
                                    ctypes.c_void_p(self.stream.cuda_stream), ctypes.byref(h)))

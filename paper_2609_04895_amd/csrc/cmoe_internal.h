@@ -207,6 +207,27 @@ constexpr int kMoeTokens = 64;      // tokens of a whole-layer call, at most: on
 constexpr int kMoeUnitTokens = 16;  // tokens of an expert in one pass over its weights: columns of a matrix-core tile
 enum MoeFormat { kMoeF32 = 0, kMoeBf16 = 1, kMoeMx8 = 2 };  // of the expert weights
 
+// Up to kMoeUnitTokens tokens of one expert.
+struct MoeUnit {
+    int32_t expert;
+    int32_t n;                      // tokens, 0 past the last unit
+    int32_t row;                    // row of the first one in act and out
+    uint8_t token[kMoeUnitTokens];  // the last one repeated past n
+};
+
+// What the router launch leaves for the expert launches, and its own counters
+// (zero between calls).
+struct MoePlan {
+    int32_t units;
+    int32_t groups_done;                                  // token groups whose selection is done
+    int32_t logits_done[kMoeTokens];                      // per token group: workgroups whose logits are done
+    MoeUnit unit[kMaxN + kMoeTokens * kMaxK / kMoeUnitTokens];
+};
+
+// Units of a call, at most: every expert with a token has one, and one more for
+// every full unit of tokens.
+constexpr int moe_max_units(int rows, int N) { return rows < N ? rows : N + rows / kMoeUnitTokens; }
+
 // One whole-layer call.
 struct MoeArgs {
     int32_t N, K, d, F, T;
@@ -228,13 +249,17 @@ struct MoeArgs {
     int32_t* selected;      // [T][K] or NULL
     float* gates;           // [T][K] or NULL
     // workspace
+    MoePlan* plan;
     float* z;               // [T][N]   logits
     int32_t* sel;           // [T][K]   selected experts, -1: none
     float* gate;            // [T][K]
+    int32_t* row_of;        // [T][K]   row of a token's expert in out, -1: none
+    int32_t* rows_done;     // [d / 16] units whose 16 outputs are done
     uint16_t* x;            // [T][d]   bf16 values of h8
     void* act;              // SwiGLU intermediate by row: [3][F] bf16 or [F] fp32
     float* out;             // [rows][d] expert outputs; a row is one (expert, token), in that order
 };
+hipError_t launch_moe_init(MoePlan* plan, hipStream_t st);  // zero counters
 hipError_t launch_moe(const MoeArgs& a, hipStream_t st);
 
 // Sets the calling thread's error text and returns the status, for entry points

@@ -114,8 +114,9 @@ bool norm_aligned(const cmoe::NormArgs& a) {
            row(a.h8, a.h8_stride, 1, 8);
 }
 
-struct MoePlan {
-    size_t z, sel, gate, h, h8, h8_scale, x, act, out, total;
+// Offsets of the workspace's parts.
+struct Parts {
+    size_t plan, z, sel, gate, row_of, rows_done, h, h8, h8_scale, x, act, out, total;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -141,8 +142,8 @@ cmoe_status check_moe(const cmoe_moe_config* c) {
     return CMOE_OK;
 }
 
-MoePlan moe_plan(const cmoe_moe_config* c) {
-    MoePlan p{};
+Parts moe_parts(const cmoe_moe_config* c) {
+    Parts p{};
     size_t o = 0;
     auto take = [&o](size_t bytes) {
         const size_t at = o;
@@ -151,9 +152,12 @@ MoePlan moe_plan(const cmoe_moe_config* c) {
     };
     const size_t T = c->T, d = c->d, rows = T * c->K, e = elem(c->dtype);
     const bool a8 = c->activations == CMOE_FORMAT_MX8;
+    p.plan = take(sizeof(cmoe::MoePlan));
     p.z = take(T * c->N * 4);
     p.sel = take(rows * 4);
     p.gate = take(rows * 4);
+    p.row_of = take(rows * 4);
+    p.rows_done = take(d / 16 * 4);
     p.h = take(T * d * e);
     p.h8 = take(a8 ? T * d : 0);
     p.h8_scale = take(a8 ? T * d / 32 : 0);
@@ -169,7 +173,7 @@ MoePlan moe_plan(const cmoe_moe_config* c) {
 struct cmoe_moe {
     cmoe_moe_config cfg;
     cmoe_moe_weights w;
-    MoePlan plan;
+    Parts parts;
     char* ws;
     hipStream_t stream;
     int device;
@@ -219,12 +223,15 @@ cmoe_status run_layer(cmoe_moe* m, const cmoe_moe_call* c, const void* h, int64_
     a.h8 = h8; a.h8_stride = h8_stride; a.h8_scale = h8_scale; a.h8_scale_stride = h8_scale_stride;
     a.y = c->y; a.y_stride = c->y_stride;
     a.n_tokens = c->n_tokens; a.selected = c->selected; a.gates = c->gates;
-    a.z = reinterpret_cast<float*>(m->ws + m->plan.z);
-    a.sel = reinterpret_cast<int32_t*>(m->ws + m->plan.sel);
-    a.gate = reinterpret_cast<float*>(m->ws + m->plan.gate);
-    a.x = reinterpret_cast<uint16_t*>(m->ws + m->plan.x);
-    a.act = m->ws + m->plan.act;
-    a.out = reinterpret_cast<float*>(m->ws + m->plan.out);
+    a.plan = reinterpret_cast<cmoe::MoePlan*>(m->ws + m->parts.plan);
+    a.row_of = reinterpret_cast<int32_t*>(m->ws + m->parts.row_of);
+    a.rows_done = reinterpret_cast<int32_t*>(m->ws + m->parts.rows_done);
+    a.z = reinterpret_cast<float*>(m->ws + m->parts.z);
+    a.sel = reinterpret_cast<int32_t*>(m->ws + m->parts.sel);
+    a.gate = reinterpret_cast<float*>(m->ws + m->parts.gate);
+    a.x = reinterpret_cast<uint16_t*>(m->ws + m->parts.x);
+    a.act = m->ws + m->parts.act;
+    a.out = reinterpret_cast<float*>(m->ws + m->parts.out);
     const hipError_t err = cmoe::launch_moe(a, m->stream);
     if (err != hipSuccess) {
         m->broken = true;
@@ -277,7 +284,7 @@ cmoe_status cmoe_moe_query(const cmoe_moe_config* cfg, size_t* workspace_bytes) 
     const cmoe_status st = check_moe(cfg);
     if (st != CMOE_OK) return st;
     if (!workspace_bytes) return fail(CMOE_ERR_INVALID_ARG, "size output is NULL");
-    *workspace_bytes = moe_plan(cfg).total;
+    *workspace_bytes = moe_parts(cfg).total;
     return CMOE_OK;
 }
 
@@ -309,10 +316,16 @@ cmoe_status cmoe_moe_init(const cmoe_moe_config* cfg, const cmoe_moe_weights* w,
     if (!m) return fail(CMOE_ERR_UNSUPPORTED, "no host memory for the handle");
     m->cfg = *cfg;
     m->w = *w;
-    m->plan = moe_plan(cfg);
+    m->parts = moe_parts(cfg);
     m->ws = static_cast<char*>(workspace);
     m->stream = static_cast<hipStream_t>(stream);
     m->device = device;
+    hipError_t e = cmoe::launch_moe_init(reinterpret_cast<cmoe::MoePlan*>(m->ws + m->parts.plan), m->stream);
+    if (e == hipSuccess) e = hipStreamSynchronize(m->stream);
+    if (e != hipSuccess) {
+        delete m;
+        return hip_fail(e, "cmoe_moe_init");
+    }
     *out = m;
     return CMOE_OK;
 }
@@ -353,12 +366,12 @@ cmoe_status cmoe_moe_block(cmoe_moe* m, const cmoe_norm* n, const cmoe_moe_call*
     cmoe::NormArgs a = norm_args(n);
     const bool a8 = g.activations == CMOE_FORMAT_MX8;
     a.n_rows = c->n_tokens;
-    a.h = m->ws + m->plan.h;
+    a.h = m->ws + m->parts.h;
     a.h_stride = g.d;
     if (a8) {
-        a.h8 = reinterpret_cast<uint8_t*>(m->ws + m->plan.h8);
+        a.h8 = reinterpret_cast<uint8_t*>(m->ws + m->parts.h8);
         a.h8_stride = g.d;
-        a.h8_scale = reinterpret_cast<uint8_t*>(m->ws + m->plan.h8_scale);
+        a.h8_scale = reinterpret_cast<uint8_t*>(m->ws + m->parts.h8_scale);
         a.h8_scale_stride = g.d / 32;
     }
     const hipError_t e = cmoe::launch_norm(a, norm_aligned(a), m->stream);
