@@ -215,12 +215,8 @@ struct MoeUnit {
     uint8_t token[kMoeUnitTokens];  // the last one repeated past n
 };
 
-// What the router launch leaves for the expert launches, and its own counters
-// (zero between calls).
+// The experts' work of a call.
 struct MoePlan {
-    int32_t units;
-    int32_t groups_done;                                  // token groups whose selection is done
-    int32_t logits_done[kMoeTokens];                      // per token group: workgroups whose logits are done
     MoeUnit unit[kMaxN + kMoeTokens * kMaxK / kMoeUnitTokens];
 };
 
@@ -251,15 +247,12 @@ struct MoeArgs {
     // workspace
     MoePlan* plan;
     float* z;               // [T][N]   logits
-    int32_t* sel;           // [T][K]   selected experts, -1: none
     float* gate;            // [T][K]
     int32_t* row_of;        // [T][K]   row of a token's expert in out, -1: none
-    int32_t* rows_done;     // [d / 16] units whose 16 outputs are done
     uint16_t* x;            // [T][d]   bf16 values of h8
     void* act;              // SwiGLU intermediate by row: [3][F] bf16 or [F] fp32
     float* out;             // [rows][d] expert outputs; a row is one (expert, token), in that order
 };
-hipError_t launch_moe_init(MoePlan* plan, hipStream_t st);  // zero counters
 hipError_t launch_moe(const MoeArgs& a, hipStream_t st);
 
 // Sets the calling thread's error text and returns the status, for entry points

@@ -116,7 +116,7 @@ bool norm_aligned(const cmoe::NormArgs& a) {
 
 // Offsets of the workspace's parts.
 struct Parts {
-    size_t plan, z, sel, gate, row_of, rows_done, h, h8, h8_scale, x, act, out, total;
+    size_t plan, z, gate, row_of, h, h8, h8_scale, x, act, out, total;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -154,10 +154,8 @@ Parts moe_parts(const cmoe_moe_config* c) {
     const bool a8 = c->activations == CMOE_FORMAT_MX8;
     p.plan = take(sizeof(cmoe::MoePlan));
     p.z = take(T * c->N * 4);
-    p.sel = take(rows * 4);
     p.gate = take(rows * 4);
     p.row_of = take(rows * 4);
-    p.rows_done = take(d / 16 * 4);
     p.h = take(T * d * e);
     p.h8 = take(a8 ? T * d : 0);
     p.h8_scale = take(a8 ? T * d / 32 : 0);
@@ -225,9 +223,7 @@ cmoe_status run_layer(cmoe_moe* m, const cmoe_moe_call* c, const void* h, int64_
     a.n_tokens = c->n_tokens; a.selected = c->selected; a.gates = c->gates;
     a.plan = reinterpret_cast<cmoe::MoePlan*>(m->ws + m->parts.plan);
     a.row_of = reinterpret_cast<int32_t*>(m->ws + m->parts.row_of);
-    a.rows_done = reinterpret_cast<int32_t*>(m->ws + m->parts.rows_done);
     a.z = reinterpret_cast<float*>(m->ws + m->parts.z);
-    a.sel = reinterpret_cast<int32_t*>(m->ws + m->parts.sel);
     a.gate = reinterpret_cast<float*>(m->ws + m->parts.gate);
     a.x = reinterpret_cast<uint16_t*>(m->ws + m->parts.x);
     a.act = m->ws + m->parts.act;
@@ -320,12 +316,6 @@ cmoe_status cmoe_moe_init(const cmoe_moe_config* cfg, const cmoe_moe_weights* w,
     m->ws = static_cast<char*>(workspace);
     m->stream = static_cast<hipStream_t>(stream);
     m->device = device;
-    hipError_t e = cmoe::launch_moe_init(reinterpret_cast<cmoe::MoePlan*>(m->ws + m->parts.plan), m->stream);
-    if (e == hipSuccess) e = hipStreamSynchronize(m->stream);
-    if (e != hipSuccess) {
-        delete m;
-        return hip_fail(e, "cmoe_moe_init");
-    }
     *out = m;
     return CMOE_OK;
 }
