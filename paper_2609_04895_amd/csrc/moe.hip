@@ -369,11 +369,27 @@ __device__ __forceinline__ void tile_product(const Tiles& tiles, const char* con
     // 8-bit rows may end in half a line: units 4 .. 7 of it would be the next row's
     const bool ragged = FORMAT == kMoeMx8 && pitch % 128 != 0;
     const char *w0 = tiles.w0 + i8 * pitch, *w1 = tiles.w1 + i8 * pitch;
+    // lane 4 i + p loads the four scales of row i and pair p, a (tile, line) of the
+    // batch: the lanes of a row's neighbouring lines share a cache lookup
+    static_assert(FORMAT != kMoeMx8 || CH * RT <= 4, "four pairs at most");
+    const int pt = (lane & 3) / CH, pl = (lane & 3) % CH;
     const uint8_t* s = nullptr;
-    if constexpr (FORMAT == kMoeMx8) s = (r < 8 ? tiles.s0 : tiles.s1) + (int64_t)(r & 7) * (pitch / 32);
+    if constexpr (FORMAT == kMoeMx8)
+        s = (lane < 32 ? tiles.s0 : tiles.s1) + (int64_t)((lane >> 2) & 7) * (pitch / 32) + pt * (tiles.next / 32) + 4 * pl;
     const char* row = stage + (r >> 3) * 1024 + (r & 7) * 128;
     for (int l = l0; l < l1; l += CH) {
-        uint32_t scales[CH][RT] = {};
+        uint32_t scales = 0;
+        if constexpr (FORMAT == kMoeMx8) {
+            if (pt < RT && l + pl < l1) {
+                if (ragged && l + pl == lines - 1) {
+                    uint16_t v;
+                    __builtin_memcpy(&v, s + 4 * l, 2);
+                    scales = v;
+                } else {
+                    __builtin_memcpy(&scales, s + 4 * l, 4);
+                }
+            }
+        }
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             if (l + i < l1) {
@@ -396,19 +412,6 @@ __device__ __forceinline__ void tile_product(const Tiles& tiles, const char* con
                         for (int k = 0; k < P::kParts; ++k)
                             if (!(half && k > 0))
                                 load_to_lds(x[j] + ((int64_t)(l + i) * P::kParts + k) * 128, stage + CH * kA + i * kB + (j * P::kParts + k) * 1024);
-                if constexpr (FORMAT == kMoeMx8) {
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-                        const uint8_t* p = s + t * (tiles.next / 32) + 4 * (l + i);
-                        if (half) {
-                            uint16_t v;
-                            __builtin_memcpy(&v, p, 2);
-                            scales[i][t] = v;
-                        } else {
-                            __builtin_memcpy(&scales[i][t], p, 4);
-                        }
-                    }
-                }
             }
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the lines are in LDS
@@ -430,8 +433,9 @@ __device__ __forceinline__ void tile_product(const Tiles& tiles, const char* con
                 for (int t = 0; t < RT; ++t) {
                     const u32x4 w[2] = {*reinterpret_cast<const u32x4*>(row + i * kA + t * 2048 + (q ^ (r & 7)) * 16),
                                         *reinterpret_cast<const u32x4*>(row + i * kA + t * 2048 + ((q + 4) ^ (r & 7)) * 16)};
+                    const uint32_t four = FORMAT == kMoeMx8 ? (uint32_t)__shfl((int)scales, 4 * r + t * CH + i) : 0u;
 #pragma unroll
-                    for (int g = 0; g < G; ++g) acc[t][g] = P::mul(w, scales[i][t], b[g], half, acc[t][g]);
+                    for (int g = 0; g < G; ++g) acc[t][g] = P::mul(w, four, b[g], half, acc[t][g]);
                 }
             }
         }
