@@ -259,17 +259,18 @@ __global__ __launch_bounds__(kThreads) void moe_logits_kernel(MoeArgs a) {
 }
 
 // ---------------------------------------------------------------- products
-// Sixteen weight rows against up to 16 G columns, the sum cut into lines of 128
-// bytes of a row.  A wavefront takes RT tiles of 16 rows and a range of the lines,
-// a few lines at a time.  An instruction brings one line of eight rows into the
-// wavefront's part of LDS, lane 8 i + p the 16-byte unit p ^ i of row i, so that
-// the reads of the operands, lane (r, q) = 16 q + r the units q and q + 4 of row
-// r, meet every LDS bank once.  The columns' values come the same way (straight
-// into registers, 16 columns cost an instruction 64 cache lookups, and the columns
-// of the down product as much time as its weights); both operands take the same
-// order of the sum.
-constexpr int kStageBytes = 16384;  // of a wavefront: two workgroups per CU, 64 KB of weights in flight
-
+// Sixteen weight rows against up to 8 NB columns, the sum cut into lines of 128
+// bytes of a row.  A wavefront takes RT tiles of 16 rows and a range of the lines.
+// An instruction loads one line of eight rows, lane 8 i + p the 16-byte unit p of
+// row i, and goes through the wavefront's part of LDS, unit p at place p ^ i of its
+// row, so that the writes, and the reads of the operands, lane (r, q) = 16 q + r
+// the units q and q + 4 of row r, meet every LDS bank once.  The columns' values
+// come the same way (straight into operand registers, 16 columns cost an
+// instruction 64 cache lookups, and the columns of the down product as much time
+// as its weights); both operands take the same order of the sum.
+//
+// The registers hold the lines in flight, CH per wavefront: line l + CH is asked
+// for when line l has gone to LDS, which holds one line at a time.
 template <int FORMAT>
 struct Format;
 
@@ -279,42 +280,36 @@ struct Format<kMoeBf16> {
     static constexpr int kParts = 1;   // 128-byte lines that these values take in a column
     static constexpr int kPlanes = 3;  // bf16 numbers of an fp32 intermediate value
     static constexpr int kBytes = 2;   // of a column's value
-    __device__ static int unit(int i, int q) { return q + 4 * i; }  // of operand read i, part 0
-    __device__ static f32x4 mul(const u32x4 (&w)[2], uint32_t, const u32x4* b, bool, f32x4 c) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[i]), __builtin_bit_cast(bf16x8, b[i]), c, 0, 0, 0);
-        return c;
+    static constexpr int kReads = 1;   // operand reads of a column per half line
+    __device__ static int unit(int i, int, int q) { return q + 4 * i; }  // of half i, read j
+    // half a line: unit w of the lane's row
+    __device__ static f32x4 mul(const u32x4& w, uint32_t, int, const u32x4* b, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, b[0]), c, 0, 0, 0);
     }
 };
 
 template <>
 struct Format<kMoeMx8> {
     static constexpr int kLine = 128, kParts = 2, kPlanes = 3, kBytes = 2;
-    // operand read i: part i / 2
-    __device__ static int unit(int i, int q) { return 2 * q + (i & 1); }
-    // The weights become bf16, in which every value is exact; scales: the line's
-    // four.  half: the line holds 64 values.
-    __device__ static f32x4 mul(const u32x4 (&w)[2], uint32_t scales, const u32x4* b, bool half, f32x4 c) {
+    static constexpr int kReads = 2;
+    __device__ static int unit(int, int j, int q) { return 2 * q + j; }  // half i is part i
+    // The weights become bf16, in which every value is exact; scales: the line's four.
+    __device__ static f32x4 mul(const u32x4& w, uint32_t scales, int i, const u32x4* b, f32x4 c) {
         const int q = (threadIdx.x & 63) >> 4;
+        const float s = __uint_as_float((scales >> (16 * i + 8 * (q >> 1)) & 255u) << 23);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (i == 1 && half) break;
-            const float s = __uint_as_float((scales >> (16 * i + 8 * (q >> 1)) & 255u) << 23);
+        for (int j = 0; j < 2; ++j) {
+            bf16x8 v;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                bf16x8 v;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i][2 * j + k], s, false);
-                    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i][2 * j + k], s, true);
-                    v[4 * k] = lo[0];
-                    v[4 * k + 1] = lo[1];
-                    v[4 * k + 2] = hi[0];
-                    v[4 * k + 3] = hi[1];
-                }
-                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, b[2 * i + j]), c, 0, 0, 0);
+            for (int k = 0; k < 2; ++k) {
+                const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * j + k], s, false);
+                const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * j + k], s, true);
+                v[4 * k] = lo[0];
+                v[4 * k + 1] = lo[1];
+                v[4 * k + 2] = hi[0];
+                v[4 * k + 3] = hi[1];
             }
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, b[j]), c, 0, 0, 0);
         }
         return c;
     }
@@ -322,29 +317,15 @@ struct Format<kMoeMx8> {
 
 template <>
 struct Format<kMoeF32> {
-    static constexpr int kLine = 32, kParts = 1, kPlanes = 1, kBytes = 4;
-    __device__ static int unit(int i, int q) { return q + 4 * i; }
-    __device__ static f32x4 mul(const u32x4 (&w)[2], uint32_t, const u32x4* b, bool, f32x4 c) {
+    static constexpr int kLine = 32, kParts = 1, kPlanes = 1, kBytes = 4, kReads = 1;
+    __device__ static int unit(int i, int, int q) { return q + 4 * i; }
+    __device__ static f32x4 mul(const u32x4& w, uint32_t, int, const u32x4* b, f32x4 c) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i][j]), __uint_as_float(b[i][j]), c, 0, 0, 0);
+        for (int j = 0; j < 4; ++j)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[j]), __uint_as_float(b[0][j]), c, 0, 0, 0);
         return c;
     }
 };
-
-using LdsBytes = __attribute__((address_space(3))) void*;
-using GlobalBytes = const __attribute__((address_space(1))) void*;
-
-// 64 times 16 bytes from each lane's address to LDS, in lane order.  Weights are
-// read once: nontemporal.
-__device__ inline void stream_to_lds(const char* p, char* lds) {
-    __builtin_amdgcn_global_load_lds((GlobalBytes)p, (LdsBytes)lds, 16, 0, 2);
-}
-__device__ inline void load_to_lds(const char* p, char* lds) {
-    __builtin_amdgcn_global_load_lds((GlobalBytes)p, (LdsBytes)lds, 16, 0, 0);
-}
 
 // A wavefront's weight tiles: rows 0 .. 7 and 8 .. 15 of a tile begin at w0 and w1,
 // `pitch` bytes apart, the next tile `next` bytes on (scales s0, s1, all distances
@@ -355,93 +336,151 @@ struct Tiles {
     int64_t pitch, next;
 };
 
-// acc[t][g] += lines l0 .. l1 of `lines` of tile t times columns 16 g .. of
-// `columns` (at least 1); x[j]: this lane's unit of part 0 of column 8 j + lane / 8.
-template <int FORMAT, int RT, int G>
-__device__ __forceinline__ void tile_product(const Tiles& tiles, const char* const (&x)[2 * G], int columns, int l0, int l1,
-                                             int lines, char* stage, f32x4 (&acc)[RT][G]) {
+// Parts of a line's columns that are held at once: both, unless there are so many
+// columns that they leave no registers for the weights.
+template <int FORMAT, int NB>
+constexpr int kHeld = NB <= 2 ? Format<FORMAT>::kParts : 1;
+
+// Bytes of LDS that a line takes with its columns.
+template <int FORMAT, int RT, int NB>
+constexpr int kLineBytes = RT * 2048 + NB * kHeld<FORMAT, NB> * 1024;
+
+template <int FORMAT, int RT, int NB>
+struct Product {
     using P = Format<FORMAT>;
-    constexpr int kA = RT * 2048, kB = G * P::kParts * 2048, CH = kStageBytes / (kA + kB);
-    static_assert(CH >= 1, "one line at least");
-    constexpr int kReads = 2 * P::kParts;
-    const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, i8 = lane >> 3, p8 = (lane & 7) ^ i8;
-    const int64_t pitch = tiles.pitch;
+    static constexpr int G = (NB + 1) / 2;  // groups of 16 columns
+    // lines in flight: 8 KB of weights where the columns leave the registers for it
+    static constexpr int CH = std::max(1, std::min(4 / RT, 8 / (NB * kHeld<FORMAT, NB>)));
+    static constexpr int kParts = kHeld<FORMAT, NB>;
+    struct Line {
+        u32x4 w[RT][2], x[NB][kParts];
+    };
+
+    const Tiles& tiles;
+    const char* const (&x)[NB];  // this lane's unit of part 0 of column 8 j + lane / 8
+    int columns, l0, l1, lines;
+    char* lds;
+    int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, i8 = lane >> 3, p8 = lane & 7;
     // 8-bit rows may end in half a line: units 4 .. 7 of it would be the next row's
-    const bool ragged = FORMAT == kMoeMx8 && pitch % 128 != 0;
-    const char *w0 = tiles.w0 + i8 * pitch, *w1 = tiles.w1 + i8 * pitch;
-    // lane 4 i + p loads the four scales of row i and pair p, a (tile, line) of the
-    // batch: the lanes of a row's neighbouring lines share a cache lookup
-    static_assert(FORMAT != kMoeMx8 || CH * RT <= 4, "four pairs at most");
-    const int pt = (lane & 3) / CH, pl = (lane & 3) % CH;
-    const uint8_t* s = nullptr;
-    if constexpr (FORMAT == kMoeMx8)
-        s = (lane < 32 ? tiles.s0 : tiles.s1) + (int64_t)((lane >> 2) & 7) * (pitch / 32) + pt * (tiles.next / 32) + 4 * pl;
-    const char* row = stage + (r >> 3) * 1024 + (r & 7) * 128;
-    for (int l = l0; l < l1; l += CH) {
-        uint32_t scales = 0;
-        if constexpr (FORMAT == kMoeMx8) {
-            if (pt < RT && l + pl < l1) {
-                if (ragged && l + pl == lines - 1) {
-                    uint16_t v;
-                    __builtin_memcpy(&v, s + 4 * l, 2);
-                    scales = v;
-                } else {
-                    __builtin_memcpy(&scales, s + 4 * l, 4);
-                }
-            }
+    bool ragged = FORMAT == kMoeMx8 && tiles.pitch % 128 != 0;
+
+    __device__ __forceinline__ bool half(int l) const { return ragged && l == lines - 1; }
+
+    __device__ __forceinline__ void load_weights(Line& v, int l) const {
+        const int64_t at = i8 * tiles.pitch + (int64_t)l * 128 + (half(l) ? p8 & 3 : p8) * 16;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            // weights are read once: nontemporal
+            v.w[t][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tiles.w0 + t * tiles.next + at));
+            v.w[t][1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tiles.w1 + t * tiles.next + at));
         }
+    }
+    // part k of the columns
+    __device__ __forceinline__ void load_columns(Line& v, int l, int k) const {
+        const int64_t at = ((int64_t)l * P::kParts + (half(l) ? 0 : k)) * 128;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            if (l + i < l1) {
-                const int64_t at = (int64_t)(l + i) * 128 + (ragged && l + i == lines - 1 ? p8 & 3 : p8) * 16;
+        for (int j = 0; j < NB; ++j) v.x[j][k % kParts] = *reinterpret_cast<const u32x4*>(x[j] + at);
+    }
+
+    // lane 4 i + p loads the four scales of row i and pair p, a (tile, line) of a
+    // batch of CH lines from l: the lanes of a row's neighbouring lines share a lookup
+    __device__ __forceinline__ uint32_t load_scales(int l) const {
+        if constexpr (FORMAT != kMoeMx8) return 0;
+        static_assert(CH * RT <= 4, "four pairs at most");
+        const int t = min((lane & 3) / CH, RT - 1), at = min(l + (lane & 3) % CH, l1 - 1);
+        const uint8_t* p = (lane < 32 ? tiles.s0 : tiles.s1) + ((lane >> 2) & 7) * (tiles.pitch / 32) + t * (tiles.next / 32) + 4 * at;
+        if (!ragged) return *reinterpret_cast<const uint32_t*>(p);
+        const uint16_t *lo = reinterpret_cast<const uint16_t*>(p), *hi = lo + (at == lines - 1 ? 0 : 1);
+        return *lo | (uint32_t)*hi << 16;
+    }
+
+    // The products of line l, held in v and number i of its batch; v then holds
+    // line `next` if there is one (a wavefront's LDS accesses stay in order).
+    __device__ __forceinline__ void step(Line& v, int l, int i, uint32_t scales, int next, f32x4 (&acc)[RT][G]) const {
+        char* to = lds + i8 * 128 + (p8 ^ i8) * 16;
+        const char *row = lds + (r >> 3) * 1024 + (r & 7) * 128, *column = lds + RT * 2048;
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    stream_to_lds(w0 + t * tiles.next + at, stage + i * kA + t * 2048);
-                    stream_to_lds(w1 + t * tiles.next + at, stage + i * kA + t * 2048 + 1024);
-                }
-            }
+        for (int t = 0; t < RT; ++t) {
+            *reinterpret_cast<u32x4*>(to + t * 2048) = v.w[t][0];
+            *reinterpret_cast<u32x4*>(to + t * 2048 + 1024) = v.w[t][1];
         }
+        if (next >= 0) load_weights(v, next);
+        uint32_t four[RT] = {};
+        if constexpr (FORMAT == kMoeMx8)
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            if (l + i < l1) {
-                const bool half = ragged && l + i == lines - 1;
+            for (int t = 0; t < RT; ++t) four[t] = (uint32_t)__shfl((int)scales, 4 * r + t * CH + i);
+        // halves of the line: both at once, or one after the other
+        constexpr int kAtOnce = kParts == P::kParts ? 2 : 1;
 #pragma unroll
-                for (int j = 0; j < 2 * G; ++j)
-                    if (8 * j < columns)
+        for (int k0 = 0; k0 < 2; k0 += kAtOnce) {
 #pragma unroll
-                        for (int k = 0; k < P::kParts; ++k)
-                            if (!(half && k > 0))
-                                load_to_lds(x[j] + ((int64_t)(l + i) * P::kParts + k) * 128, stage + CH * kA + i * kB + (j * P::kParts + k) * 1024);
+            for (int k = 0; k < kParts; ++k)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) *reinterpret_cast<u32x4*>(to + RT * 2048 + (j * kParts + k) * 1024) = v.x[j][k];
+            if (kAtOnce == 2) {
+#pragma unroll
+                for (int k = 0; k < kParts; ++k)
+                    if (next >= 0) load_columns(v, next, k);
+            } else if (k0 == 0) {
+                load_columns(v, l, 1);
+            } else if (next >= 0) {
+                load_columns(v, next, 0);
             }
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the lines are in LDS
+            __builtin_amdgcn_wave_barrier();
+            if (k0 == 1 && half(l)) break;
+            u32x4 b[kAtOnce][G][P::kReads], w[RT][kAtOnce];
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            if (l + i < l1) {
-                const bool half = ragged && l + i == lines - 1;
-                u32x4 b[G][kReads];
+            for (int k = 0; k < kAtOnce; ++k) {
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
                     const int c = min(16 * g + r, columns - 1);  // columns past the last repeat it, and are dropped
 #pragma unroll
-                    for (int j = 0; j < kReads; ++j)
-                        if (!(half && j >= kReads / 2))
-                            b[g][j] = *reinterpret_cast<const u32x4*>(stage + CH * kA + i * kB + ((c >> 3) * P::kParts + j / 2) * 1024 +
-                                                                      (c & 7) * 128 + (P::unit(j, q) ^ (c & 7)) * 16);
+                    for (int j = 0; j < P::kReads; ++j)
+                        b[k][g][j] = *reinterpret_cast<const u32x4*>(column + ((c >> 3) * kParts + k % kParts) * 1024 + (c & 7) * 128 +
+                                                                     (P::unit(k0 + k, j, q) ^ (c & 7)) * 16);
                 }
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    const u32x4 w[2] = {*reinterpret_cast<const u32x4*>(row + i * kA + t * 2048 + (q ^ (r & 7)) * 16),
-                                        *reinterpret_cast<const u32x4*>(row + i * kA + t * 2048 + ((q + 4) ^ (r & 7)) * 16)};
-                    const uint32_t four = FORMAT == kMoeMx8 ? (uint32_t)__shfl((int)scales, 4 * r + t * CH + i) : 0u;
-#pragma unroll
-                    for (int g = 0; g < G; ++g) acc[t][g] = P::mul(w, four, b[g], half, acc[t][g]);
-                }
+                for (int t = 0; t < RT; ++t)
+                    w[t][k] = *reinterpret_cast<const u32x4*>(row + t * 2048 + ((q + 4 * (k0 + k)) ^ (r & 7)) * 16);
             }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                if (k == 1 && half(l)) break;
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) acc[t][g] = P::mul(w[t][k], four[t], k0 + k, b[k][g], acc[t][g]);
+            }
+            __builtin_amdgcn_wave_barrier();
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // and read before the next ones come
     }
-}
+
+    // acc[t][g] += lines l0 .. l1 of `lines` of tile t times columns 16 g .. of
+    // `columns` (at least 1).
+    __device__ __forceinline__ void run(f32x4 (&acc)[RT][G]) const {
+        if (l0 >= l1) return;
+        Line v[CH];
+        uint32_t scales = load_scales(l0);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int l = min(l0 + i, l1 - 1);
+            load_weights(v[i], l);
+#pragma unroll
+            for (int k = 0; k < kParts; ++k) load_columns(v[i], l, k);
+        }
+        int l = l0;
+        for (; l + 2 * CH <= l1; l += CH) {
+            const uint32_t next = load_scales(l + CH);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) step(v[i], l + i, i, scales, l + i + CH, acc);
+            scales = next;
+        }
+        const uint32_t next = l + CH < l1 ? load_scales(l + CH) : 0;
+#pragma unroll
+        for (int i = 0; i < 2 * CH - 1; ++i)
+            if (l + i < l1) step(v[i % CH], l + i, i % CH, i < CH ? scales : next, l + i + CH < l1 ? l + i + CH : -1, acc);
+    }
+};
 
 __device__ inline float silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
 
@@ -458,10 +497,26 @@ __device__ inline void split3(float v, __bf16* p) {
 // and the same eight of W_up; a workgroup takes RT of them, its wavefronts a
 // quarter of the sum each.
 // grid: x = F / (8 RT), y = units
-template <int FORMAT, int RT>
-__global__ __launch_bounds__(kThreads, 2) void moe_up_kernel(MoeArgs a) {
+template <int FORMAT, int RT, int NB>
+__device__ __forceinline__ void up_product(const MoeArgs& a, const MoeUnit& unit, int n, const Tiles& tiles, int l0, int l1, int lines,
+                                           char* lds, f32x4 (*red)[64]) {
     using P = Format<FORMAT>;
-    __shared__ __align__(16) char stage[kWaves][kStageBytes];
+    const int lane = threadIdx.x & 63, i8 = lane >> 3;
+    const char* x[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+        x[j] = (a.h8 ? reinterpret_cast<const char*>(a.x) : static_cast<const char*>(a.h)) +
+               unit.token[8 * j + i8] * (a.h8 ? (int64_t)a.d : a.h_stride) * P::kBytes + (lane & 7) * 16;
+    f32x4 acc[RT][1] = {};
+    Product<FORMAT, RT, NB>{tiles, x, n, l0, l1, lines, lds}.run(acc);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) red[t][lane] = acc[t][0];
+}
+
+template <int FORMAT, int RT>
+__global__ __launch_bounds__(kThreads, 3) void moe_up_kernel(MoeArgs a) {
+    using P = Format<FORMAT>;
+    __shared__ __align__(16) char lds[kWaves][kLineBytes<FORMAT, RT, 2>];
     __shared__ f32x4 red[kWaves][RT][64];
     const MoeUnit& unit = a.plan->unit[blockIdx.y];
     const int n = unit.n;
@@ -476,16 +531,11 @@ __global__ __launch_bounds__(kThreads, 2) void moe_up_kernel(MoeArgs a) {
     tiles.s1 = FORMAT == kMoeMx8 ? tiles.s0 + a.F * (pitch / 32) : nullptr;
     tiles.pitch = pitch;
     tiles.next = 8 * pitch;
-    const int lines = (a.d + P::kLine - 1) / P::kLine, i8 = lane >> 3, p8 = (lane & 7) ^ i8;
-    const char* x[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-        x[j] = (a.h8 ? reinterpret_cast<const char*>(a.x) : static_cast<const char*>(a.h)) +
-               unit.token[8 * j + i8] * (a.h8 ? (int64_t)a.d : a.h_stride) * P::kBytes + p8 * 16;
-    f32x4 acc[RT][1] = {};
-    tile_product<FORMAT, RT, 1>(tiles, x, n, wv * lines / kWaves, (wv + 1) * lines / kWaves, lines, stage[wv], acc);
-#pragma unroll
-    for (int t = 0; t < RT; ++t) red[wv][t][lane] = acc[t][0];
+    const int lines = (a.d + P::kLine - 1) / P::kLine, l0 = wv * lines / kWaves, l1 = (wv + 1) * lines / kWaves;
+    if (n <= 8)
+        up_product<FORMAT, RT, 1>(a, unit, n, tiles, l0, l1, lines, lds[wv], red[wv]);
+    else
+        up_product<FORMAT, RT, 2>(a, unit, n, tiles, l0, l1, lines, lds[wv], red[wv]);
     __syncthreads();
     // lane (c, q) of a product holds rows 4 q .. of column c: q = 0, 1 W_gate's, 2, 3 W_up's
     if (wv >= RT || lane >= 32 || r >= n) return;
@@ -536,21 +586,23 @@ __global__ __launch_bounds__(kThreads) void moe_sum_kernel(MoeArgs a) {
     *reinterpret_cast<f32x4*>(a.y + (int64_t)t * a.y_stride + j) = y;
 }
 
-// The down product of a unit in G groups of 16 columns: column i is bf16 number
-// i / n of token i % n's intermediate, so that up to five tokens take one group.
-template <int FORMAT, int RT, int G>
+// The down product of a unit in NB blocks of 8 columns: column i is bf16 number
+// i / n of token i % n's intermediate, so that up to five tokens take one group
+// of 16.
+template <int FORMAT, int RT, int NB>
 __device__ __forceinline__ void down_product(const MoeArgs& a, int row, int n, const Tiles& tiles, int l0, int l1, int lines,
-                                             char* stage, f32x4 (*red)[Format<FORMAT>::kPlanes][64]) {
+                                             char* lds, f32x4 (*red)[Format<FORMAT>::kPlanes][64]) {
     using P = Format<FORMAT>;
-    const int lane = threadIdx.x & 63, i8 = lane >> 3, p8 = (lane & 7) ^ i8, columns = P::kPlanes * n;
-    const char* x[2 * G];
+    constexpr int G = (NB + 1) / 2;
+    const int lane = threadIdx.x & 63, i8 = lane >> 3, columns = P::kPlanes * n;
+    const char* x[NB];
 #pragma unroll
-    for (int j = 0; j < 2 * G; ++j) {
+    for (int j = 0; j < NB; ++j) {
         const int i = min(8 * j + i8, columns - 1), plane = (i >= n) + (i >= 2 * n);
-        x[j] = static_cast<const char*>(a.act) + ((int64_t)(row + i - plane * n) * P::kPlanes + plane) * a.F * P::kBytes + p8 * 16;
+        x[j] = static_cast<const char*>(a.act) + ((int64_t)(row + i - plane * n) * P::kPlanes + plane) * a.F * P::kBytes + (lane & 7) * 16;
     }
     f32x4 acc[RT][G] = {};
-    tile_product<FORMAT, RT, G>(tiles, x, columns, l0, l1, lines, stage, acc);
+    Product<FORMAT, RT, NB>{tiles, x, columns, l0, l1, lines, lds}.run(acc);
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll
@@ -561,13 +613,12 @@ __device__ __forceinline__ void down_product(const MoeArgs& a, int row, int n, c
 // of the sum each, `split` parts.
 // grid: x = d / 16 / (RT kWaves / split) rounded up, y = units
 template <int FORMAT, int RT>
-__global__ __launch_bounds__(kThreads, 2) void moe_down_kernel(MoeArgs a, int split) {
+__global__ __launch_bounds__(kThreads, 3) void moe_down_kernel(MoeArgs a, int split) {
     using P = Format<FORMAT>;
-    constexpr int kGroups = P::kPlanes;
-    __shared__ __align__(16) char stage[kWaves][kStageBytes];
-    // the products, in the place of the lines
-    auto red = [&](int w) { return reinterpret_cast<f32x4(*)[kGroups][64]>(stage[w]); };
-    static_assert(RT * kGroups * 1024 <= kStageBytes, "the products fit");
+    constexpr int kGroups = P::kPlanes, kBlocks = 2 * kGroups;
+    // a line with its columns, then the products
+    __shared__ __align__(16) char lds[kWaves][std::max(kLineBytes<FORMAT, RT, kBlocks>, RT * kGroups * 1024)];
+    auto red = [&](int w) { return reinterpret_cast<f32x4(*)[kGroups][64]>(lds[w]); };
     const MoeUnit& unit = a.plan->unit[blockIdx.y];
     const int n = unit.n;
     if (n == 0) return;
@@ -584,14 +635,16 @@ __global__ __launch_bounds__(kThreads, 2) void moe_down_kernel(MoeArgs a, int sp
         tiles.pitch = pitch;
         tiles.next = 16 * pitch;
         const int lines = (a.F + P::kLine - 1) / P::kLine, l0 = part * lines / split, l1 = (part + 1) * lines / split;
-        const int groups = (P::kPlanes * n + 15) / 16;
-        if (groups == 1)
-            down_product<FORMAT, RT, 1>(a, unit.row, n, tiles, l0, l1, lines, stage[wv], red(wv));
+        const int columns = P::kPlanes * n;
+        if (columns <= 8)
+            down_product<FORMAT, RT, 1>(a, unit.row, n, tiles, l0, l1, lines, lds[wv], red(wv));
+        else if (columns <= 16)
+            down_product<FORMAT, RT, 2>(a, unit.row, n, tiles, l0, l1, lines, lds[wv], red(wv));
         else if constexpr (kGroups > 1) {
-            if (groups == 2)
-                down_product<FORMAT, RT, 2>(a, unit.row, n, tiles, l0, l1, lines, stage[wv], red(wv));
+            if (columns <= 32)
+                down_product<FORMAT, RT, 4>(a, unit.row, n, tiles, l0, l1, lines, lds[wv], red(wv));
             else
-                down_product<FORMAT, RT, 3>(a, unit.row, n, tiles, l0, l1, lines, stage[wv], red(wv));
+                down_product<FORMAT, RT, 6>(a, unit.row, n, tiles, l0, l1, lines, lds[wv], red(wv));
         }
     }
     __syncthreads();
