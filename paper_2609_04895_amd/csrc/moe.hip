@@ -404,7 +404,6 @@ struct Product {
             *reinterpret_cast<u32x4*>(to + t * 2048) = v.w[t][0];
             *reinterpret_cast<u32x4*>(to + t * 2048 + 1024) = v.w[t][1];
         }
-        if (next >= 0) load_weights(v, next);
         uint32_t four[RT] = {};
         if constexpr (FORMAT == kMoeMx8)
 #pragma unroll
@@ -417,10 +416,11 @@ struct Product {
             for (int k = 0; k < kParts; ++k)
 #pragma unroll
                 for (int j = 0; j < NB; ++j) *reinterpret_cast<u32x4*>(to + RT * 2048 + (j * kParts + k) * 1024) = v.x[j][k];
+            if (k0 == 0 && next >= 0) load_weights(v, next);
             if (kAtOnce == 2) {
+                if (next >= 0)
 #pragma unroll
-                for (int k = 0; k < kParts; ++k)
-                    if (next >= 0) load_columns(v, next, k);
+                    for (int k = 0; k < kParts; ++k) load_columns(v, next, k);
             } else if (k0 == 0) {
                 load_columns(v, l, 1);
             } else if (next >= 0) {
