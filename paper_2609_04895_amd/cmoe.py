@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -150,12 +151,12 @@ def lib():
         L.cmoe_concentration.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double)]
         L.cmoe_read_probe.argtypes = [vp, ctypes.c_int64, i32, ctypes.POINTER(ctypes.c_double)]
         i64, ref = ctypes.c_int64, ctypes.POINTER
-        L.cmoe_add_norm.argtypes = [ref(cmoe_norm), vp]
+        L.cmoe_add_norm.argtypes = [vp, vp]  # cmoe_norm, as a structure or its bytes
         L.cmoe_quantize.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, vp]
         L.cmoe_moe_query.argtypes = [ref(cmoe_moe_config), ref(ctypes.c_size_t)]
         L.cmoe_moe_init.argtypes = [ref(cmoe_moe_config), ref(cmoe_moe_weights), vp, vp, ref(vp)]
-        L.cmoe_moe_layer.argtypes = [vp, ref(cmoe_moe_call)]
-        L.cmoe_moe_block.argtypes = [vp, ref(cmoe_norm), ref(cmoe_moe_call)]
+        L.cmoe_moe_layer.argtypes = [vp, vp]
+        L.cmoe_moe_block.argtypes = [vp, vp, vp]
         L.cmoe_moe_destroy.argtypes = [vp]
         L.cmoe_last_error.argtypes = []
         L.cmoe_last_error.restype = ctypes.c_char_p
@@ -337,64 +338,84 @@ class Engine:
 
 
 # ------------------------------------------------------------ operators without a cache
+# A call of these takes as little as a few microseconds of the device, so their
+# arguments are checked and packed with as few Python steps as it takes: one
+# structure as bytes, addresses and the current stream as plain integers.
+_NORM = struct.Struct("iiiif4x" + "q" * 14)  # cmoe_norm
+_CALL = struct.Struct("ii" + "q" * 11)       # cmoe_moe_call
+
+
+def _torch():
+    """torch, and the cmoe_dtype of its types (torch is imported on first use)."""
+    global _torch_types
+    if _torch_types is None:
+        import torch
+        _torch_types = (torch, {torch.float32: CMOE_F32, torch.bfloat16: CMOE_BF16})
+    return _torch_types
+
+
+_torch_types = None
+
+
 def _invalid(msg):
     raise CmoeError(CMOE_ERR_INVALID_ARG, msg)
 
 
-def _rows(t, name, dtype, rows, cols, device):
-    """Address and row stride of a device tensor [rows][cols] whose rows are
-    contiguous; raises on any other tensor."""
-    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.device != device:
-        _invalid(f"{name} must be a [{rows}][{cols}] tensor of {dtype} on {device}")
-    if cols > 1 and t.stride(1) != 1:
+def _rows(t, name, dtype, shape, dev):
+    """Address and row stride of a tensor [rows][cols] of device `dev` whose rows
+    are contiguous; raises on any other tensor."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        _invalid(f"{name} must be a {list(shape)} tensor of {dtype} on the other tensors' device")
+    row, col = t.stride()
+    if col != 1 and shape[1] > 1:
         _invalid(f"the rows of {name} must be contiguous")
-    return t.data_ptr(), (t.stride(0) if rows > 1 else cols)
+    return t.data_ptr(), (row if shape[0] > 1 else shape[1])
 
 
-def _flat(t, name, dtype, numel, device):
-    if t.dtype != dtype or t.numel() != numel or not t.is_contiguous() or t.device != device:
-        _invalid(f"{name} must be a contiguous tensor of {numel} values of {dtype} on {device}")
+def _flat(t, name, dtype, numel, dev):
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != dev:
+        _invalid(f"{name} must be a contiguous tensor of {numel} values of {dtype} on the other tensors' device")
     return t.data_ptr()
 
 
-def _types():
-    import torch
-    return {torch.float32: CMOE_F32, torch.bfloat16: CMOE_BF16}
-
-
-def _stream_of(torch, stream, device):
-    """hipStream_t of `stream`, or of the current stream; the work goes to the
-    current device, so the tensors have to be there."""
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
+def _on_current(torch, dev):
+    """The work goes to the current device, so the tensors have to be there."""
+    if dev < 0 or dev != torch._C._cuda_getDevice():
         _invalid("the tensors must be on the current device")
-    return (stream if stream is not None else torch.cuda.current_stream()).cuda_stream
+
+
+def _stream_of(torch, stream, dev):
+    """hipStream_t of `stream`, or of the current stream."""
+    _on_current(torch, dev)
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(dev)
 
 
 def _norm_args(residual, delta, weight, eps, residual_out, h, h8, h8_scale, n_rows):
-    import torch
-    if residual.dim() != 2 or residual.dtype not in _types():
+    torch, types = _torch()
+    dt, shape, dev = residual.dtype, residual.shape, residual.get_device()
+    if dt not in types or len(shape) != 2:
         _invalid("residual must be a [rows][d] tensor of float32 or bfloat16")
-    (rows, d), dt, dev = residual.shape, residual.dtype, residual.device
-    a = cmoe_norm(rows=rows, d=d, dtype=_types()[dt], eps=eps)
-    a.residual, a.residual_stride = _rows(residual, "residual", dt, rows, d, dev)
+    rows, d = shape
+    p, ps = _rows(residual, "residual", dt, shape, dev)
+    delta_dtype = pd = pds = po = pos = pw = ph = phs = p8 = p8s = pc = pcs = pn = 0
     if delta is not None:
-        if delta.dtype not in _types():
+        delta_dtype = types.get(delta.dtype, -1)
+        if delta_dtype < 0:
             _invalid("delta must be float32 or bfloat16")
-        a.delta_dtype = _types()[delta.dtype]
-        a.delta, a.delta_stride = _rows(delta, "delta", delta.dtype, rows, d, dev)
-    if weight is not None:
-        a.weight = _flat(weight, "weight", dt, d, dev)
+        pd, pds = _rows(delta, "delta", delta.dtype, shape, dev)
     if residual_out is not None:
-        a.residual_out, a.residual_out_stride = _rows(residual_out, "residual_out", dt, rows, d, dev)
+        po, pos = _rows(residual_out, "residual_out", dt, shape, dev)
+    if weight is not None:
+        pw = _flat(weight, "weight", dt, d, dev)
     if h is not None:
-        a.h, a.h_stride = _rows(h, "h", dt, rows, d, dev)
+        ph, phs = _rows(h, "h", dt, shape, dev)
     if h8 is not None:
-        a.h8, a.h8_stride = _rows(h8, "h8", torch.uint8, rows, d, dev)
+        p8, p8s = _rows(h8, "h8", torch.uint8, shape, dev)
     if h8_scale is not None:
-        a.h8_scale, a.h8_scale_stride = _rows(h8_scale, "h8_scale", torch.uint8, rows, d // 32, dev)
+        pc, pcs = _rows(h8_scale, "h8_scale", torch.uint8, (rows, d // 32), dev)
     if n_rows is not None:
-        a.n_rows = _flat(n_rows, "n_rows", torch.int32, 1, dev)
-    return a
+        pn = _flat(n_rows, "n_rows", torch.int32, 1, dev)
+    return _NORM.pack(rows, d, types[dt], delta_dtype, eps, p, ps, pd, pds, po, pos, pw, ph, phs, p8, p8s, pc, pcs, pn)
 
 
 def cmoe_add_norm(residual, delta=None, weight=None, eps=1e-6, residual_out=None, h=None, h8=None, h8_scale=None,
@@ -402,30 +423,33 @@ def cmoe_add_norm(residual, delta=None, weight=None, eps=1e-6, residual_out=None
     """The residual's addition and RMS norm (see the header) of [rows][d]
     tensors into the outputs given, on `stream` or the current one.  residual_out
     may be residual."""
-    import torch
     a = _norm_args(residual, delta, weight, eps, residual_out, h, h8, h8_scale, n_rows)
-    _check(lib().cmoe_add_norm(a, _stream_of(torch, stream, residual.device)))
+    st = lib().cmoe_add_norm(a, _stream_of(_torch()[0], stream, residual.get_device()))
+    if st:
+        _check(st)
 
 
 def cmoe_quantize(src, q, scale, stream=None):
     """[rows][cols] values of float32 or bfloat16 into 8 bits: q [rows][cols]
     and scale [rows][cols / 32], both uint8."""
-    import torch
-    if src.dim() != 2 or src.dtype not in _types():
+    torch, types = _torch()
+    dt, shape, dev = src.dtype, src.shape, src.get_device()
+    if dt not in types or len(shape) != 2:
         _invalid("src must be a [rows][cols] tensor of float32 or bfloat16")
-    rows, cols = src.shape
-    p, stride = _rows(src, "src", src.dtype, rows, cols, src.device)
-    pq, q_stride = _rows(q, "q", torch.uint8, rows, cols, src.device)
-    ps, s_stride = _rows(scale, "scale", torch.uint8, rows, cols // 32, src.device)
-    _check(lib().cmoe_quantize(p, _types()[src.dtype], rows, cols, stride, pq, q_stride, ps, s_stride,
-                               _stream_of(torch, stream, src.device)))
+    rows, cols = shape
+    p, stride = _rows(src, "src", dt, shape, dev)
+    pq, q_stride = _rows(q, "q", torch.uint8, shape, dev)
+    ps, s_stride = _rows(scale, "scale", torch.uint8, (rows, cols // 32), dev)
+    st = lib().cmoe_quantize(p, types[dt], rows, cols, stride, pq, q_stride, ps, s_stride, _stream_of(torch, stream, dev))
+    if st:
+        _check(st)
 
 
 def quantize_experts(experts):
     """A pool [L][N][3 d F] in 8 bits: (values, scales) [L][N][3 d F] and
     [L][N][3 d F / 32], for MoeLayers with CMOE_FORMAT_MX8."""
-    import torch
-    if not experts.is_contiguous() or experts.dim() != 3:
+    torch, _ = _torch()
+    if experts.dim() != 3 or not experts.is_contiguous() or experts.shape[2] % 32:
         _invalid("experts must be a contiguous [L][N][3 d F] tensor")
     L, N, n = experts.shape
     q = torch.empty((L, N, n), dtype=torch.uint8, device=experts.device)
@@ -453,11 +477,11 @@ class MoeLayers:
 
     def __init__(self, cfg: cmoe_moe_config, w_router, logit_bias, experts, expert_scales=None, norm_weight=None,
                  norm_eps=1e-6, stream=None):
-        import torch
         self.handle = None
-        self.cfg = cfg
+        torch, _ = _torch()
         size = cmoe_moe_query(cfg)
-        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.cfg, self.K, self.d, self.L = cfg, cfg.K, cfg.d, cfg.L
+        self.device = torch.cuda.current_device()
         self.dtype = torch.bfloat16 if cfg.dtype == CMOE_BF16 else torch.float32
         n = cfg.L * cfg.N * 3 * cfg.d * cfg.F
         mx8 = cfg.weights == CMOE_FORMAT_MX8
@@ -471,55 +495,58 @@ class MoeLayers:
             w.expert_scales = _flat(expert_scales, "expert_scales", torch.uint8, n // 32, self.device)
         if norm_weight is not None:
             _flat(norm_weight, "norm_weight", self.dtype, cfg.L * cfg.d, self.device)
-            norm_weight = norm_weight.view(cfg.L, cfg.d)
+            norm_weight = list(norm_weight.view(cfg.L, cfg.d))
         self.norm_weight, self.norm_eps = norm_weight, norm_eps
         self._keep = (w_router, logit_bias, experts, expert_scales)
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         with torch.cuda.stream(self.stream):  # the allocator's owner of the memory: the stream that uses it
-            self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
+            self.workspace = torch.empty(size, dtype=torch.uint8, device="cuda")
         h = ctypes.c_void_p()
         _check(lib().cmoe_moe_init(ctypes.byref(cfg), ctypes.byref(w), self.workspace.data_ptr(),
-                                   ctypes.c_void_p(self.stream.cuda_stream), ctypes.byref(h)))
+                                   self.stream.cuda_stream, ctypes.byref(h)))
         self.handle = h
 
-    def _call(self, layer, T, y, n_tokens, selected, gates):
-        import torch
-        cfg, dev = self.cfg, self.device
-        c = cmoe_moe_call(layer=layer, T=T)
-        c.y, c.y_stride = _rows(y, "y", torch.float32, T, cfg.d, dev)
+    def _call(self, layer, rows, h, h8, h8_scale, y, n_tokens, selected, gates):
+        torch, _ = _torch()
+        dev, d = self.device, self.d
+        shape = (rows, d)
+        ph = phs = p8 = p8s = pc = pcs = pn = psel = pg = 0
+        if h is not None:
+            ph, phs = _rows(h, "h", self.dtype, shape, dev)
+        if h8 is not None:
+            p8, p8s = _rows(h8, "h8", torch.uint8, shape, dev)
+        if h8_scale is not None:
+            pc, pcs = _rows(h8_scale, "h8_scale", torch.uint8, (rows, d // 32), dev)
+        py, pys = _rows(y, "y", torch.float32, shape, dev)
         if n_tokens is not None:
-            c.n_tokens = _flat(n_tokens, "n_tokens", torch.int32, 1, dev)
+            pn = _flat(n_tokens, "n_tokens", torch.int32, 1, dev)
         if selected is not None:
-            c.selected = _flat(selected, "selected", torch.int32, T * cfg.K, dev)
+            psel = _flat(selected, "selected", torch.int32, rows * self.K, dev)
         if gates is not None:
-            c.gates = _flat(gates, "gates", torch.float32, T * cfg.K, dev)
-        return c
+            pg = _flat(gates, "gates", torch.float32, rows * self.K, dev)
+        return _CALL.pack(layer, rows, ph, phs, p8, p8s, pc, pcs, py, pys, pn, psel, pg)
 
     def cmoe_moe_layer(self, layer, h, y, h8=None, h8_scale=None, n_tokens=None, selected=None, gates=None):
         """y [T][d] = the layer's output for the hidden states h [T][d]; the
         rows of both may be apart.  h8 and h8_scale: the experts' input with
         8-bit activations.  selected, gates: [T][K]."""
-        import torch
-        d, T = self.cfg.d, h.shape[0]
-        c = self._call(layer, T, y, n_tokens, selected, gates)
-        c.h, c.h_stride = _rows(h, "h", self.dtype, T, d, self.device)
-        if h8 is not None:
-            c.h8, c.h8_stride = _rows(h8, "h8", torch.uint8, T, d, self.device)
-        if h8_scale is not None:
-            c.h8_scale, c.h8_scale_stride = _rows(h8_scale, "h8_scale", torch.uint8, T, d // 32, self.device)
-        _check(lib().cmoe_moe_layer(self.handle, c))
+        c = self._call(layer, h.shape[0], h, h8, h8_scale, y, n_tokens, selected, gates)
+        st = lib().cmoe_moe_layer(self.handle, c)
+        if st:
+            _check(st)
 
     def cmoe_moe_block(self, layer, residual, delta, y, residual_out=None, n_tokens=None, selected=None, gates=None):
         """Norm of residual + delta (None: of the residual), then the layer."""
-        cfg = self.cfg
-        if not 0 <= layer < cfg.L:
+        if not 0 <= layer < self.L:
             _invalid("layer must be in [0, L)")
         w = None if self.norm_weight is None else self.norm_weight[layer]
         n = _norm_args(residual, delta, w, self.norm_eps, residual_out, None, None, None, None)
-        if residual.device != self.device:
-            _invalid(f"residual must be on {self.device}")
-        c = self._call(layer, residual.shape[0], y, n_tokens, selected, gates)
-        _check(lib().cmoe_moe_block(self.handle, n, c))
+        if residual.get_device() != self.device:
+            _invalid("residual must be on the handle's device")
+        c = self._call(layer, residual.shape[0], None, None, None, y, n_tokens, selected, gates)
+        st = lib().cmoe_moe_block(self.handle, n, c)
+        if st:
+            _check(st)
 
     def cmoe_moe_destroy(self):
         if self.handle is not None:

@@ -96,9 +96,10 @@ __device__ inline float key_logit(uint32_t k) {
     return k == 0xFFFFFFFFu ? NAN : __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
 
-// The selection and gates of token t, by one wavefront: lane k ends with the
-// k-th largest logit and its expert.  Returns lane k's expert, -1: none.
-__device__ inline int select_experts(const MoeArgs& a, int t, int lane) {
+// The first `count` experts of token t's selection, by one wavefront: lane k gets
+// that of the k-th largest logit, or -1 (none) for a logit of -inf.  With all K of
+// them it can write the gates and the outputs.
+__device__ inline int select_experts(const MoeArgs& a, int t, int lane, int count, bool write) {
     uint32_t key[kMaxN / 64];
 #pragma unroll
     for (int j = 0; j < kMaxN / 64; ++j) {
@@ -107,7 +108,7 @@ __device__ inline int select_experts(const MoeArgs& a, int t, int lane) {
     }
     uint32_t mine = 0;
     int expert = -1;
-    for (int k = 0; k < a.K; ++k) {
+    for (int k = 0; k < count; ++k) {
         const uint32_t m = wave_max(max(max(key[0], key[1]), max(key[2], key[3])));
         int e = -1;
 #pragma unroll
@@ -122,9 +123,10 @@ __device__ inline int select_experts(const MoeArgs& a, int t, int lane) {
             expert = e;
         }
     }
-    const float z = mine ? key_logit(mine) : -INFINITY, top = __shfl(z, 0);
+    const float z = mine ? key_logit(mine) : -INFINITY;
     const bool none = z == -INFINITY;
-    const float p = none ? 0.0f : expf(z - top);
+    if (!write) return none ? -1 : expert;
+    const float top = __shfl(z, 0), p = none ? 0.0f : expf(z - top);
     float s = p;
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
@@ -152,7 +154,7 @@ __global__ __launch_bounds__(kPlanThreads) void moe_plan_kernel(MoeArgs a) {
     if (tid < kMaxN) mask[tid] = 0;
     __syncthreads();
     for (int t = tid >> 6; t < a.T; t += kPlanThreads / 64) {
-        const int e = t < n ? select_experts(a, t, lane) : -1;
+        const int e = t < n ? select_experts(a, t, lane, a.K, true) : -1;
         if (lane < a.K) {
             sel[t * a.K + lane] = (int16_t)e;
             if (e >= 0) atomicOr(&mask[e], 1ull << t);
@@ -493,12 +495,8 @@ __device__ inline void split3(float v, __bf16* p) {
     p[2] = (__bf16)(r - (float)p[1]);
 }
 
-// Gate and up projections and the SwiGLU product: a tile is eight rows of W_gate
-// and the same eight of W_up; a workgroup takes RT of them, its wavefronts a
-// quarter of the sum each.
-// grid: x = F / (8 RT), y = units
 template <int FORMAT, int RT, int NB>
-__device__ __forceinline__ void up_product(const MoeArgs& a, const MoeUnit& unit, int n, const Tiles& tiles, int l0, int l1, int lines,
+__device__ __forceinline__ void up_product(const MoeArgs& a, const uint8_t* token, int n, const Tiles& tiles, int l0, int l1, int lines,
                                            char* lds, f32x4 (*red)[64]) {
     using P = Format<FORMAT>;
     const int lane = threadIdx.x & 63, i8 = lane >> 3;
@@ -506,24 +504,50 @@ __device__ __forceinline__ void up_product(const MoeArgs& a, const MoeUnit& unit
 #pragma unroll
     for (int j = 0; j < NB; ++j)
         x[j] = (a.h8 ? reinterpret_cast<const char*>(a.x) : static_cast<const char*>(a.h)) +
-               unit.token[8 * j + i8] * (a.h8 ? (int64_t)a.d : a.h_stride) * P::kBytes + (lane & 7) * 16;
+               (token ? token[8 * j + i8] : 0) * (a.h8 ? (int64_t)a.d : a.h_stride) * P::kBytes + (lane & 7) * 16;
     f32x4 acc[RT][1] = {};
     Product<FORMAT, RT, NB>{tiles, x, n, l0, l1, lines, lds}.run(acc);
 #pragma unroll
     for (int t = 0; t < RT; ++t) red[t][lane] = acc[t][0];
 }
 
-template <int FORMAT, int RT>
+// Gate and up projections and the SwiGLU product: a tile is eight rows of W_gate
+// and the same eight of W_up; a workgroup takes RT of them, its wavefronts a
+// quarter of the sum each.  ONE: there is one token, whose k-th expert is unit k:
+// every wavefront finds its own from the logits, which takes less than the plan's
+// launch, and one of them leaves the plan for the down projection.
+// grid: x = F / (8 RT), y = units
+template <int FORMAT, int RT, bool ONE>
 __global__ __launch_bounds__(kThreads, 3) void moe_up_kernel(MoeArgs a) {
     using P = Format<FORMAT>;
-    __shared__ __align__(16) char lds[kWaves][kLineBytes<FORMAT, RT, 2>];
+    __shared__ __align__(16) char lds[kWaves][kLineBytes<FORMAT, RT, ONE ? 1 : 2>];
     __shared__ f32x4 red[kWaves][RT][64];
-    const MoeUnit& unit = a.plan->unit[blockIdx.y];
-    const int n = unit.n;
-    if (n == 0) return;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
+    MoeUnit* unit = a.plan->unit + blockIdx.y;
+    int expert, n, row0;
+    if constexpr (ONE) {
+        const bool write = blockIdx.x == 0 && blockIdx.y == 0 && wv == 0;
+        if (live_tokens(a) == 0) {
+            if (write && lane < a.K) a.plan->unit[lane].n = 0;
+            return;
+        }
+        const int e = select_experts(a, 0, lane, write ? a.K : blockIdx.y + 1, write);
+        if (write && lane < a.K) {
+            unit[lane].expert = e;
+            unit[lane].n = e >= 0;
+            unit[lane].row = lane;
+        }
+        expert = __builtin_amdgcn_readlane(e, blockIdx.y);
+        n = expert >= 0;
+        row0 = blockIdx.y;
+    } else {
+        expert = unit->expert;
+        n = unit->n;
+        row0 = unit->row;
+    }
+    if (n == 0) return;
     const int64_t pitch = (int64_t)a.d * 128 / P::kLine;  // bytes of a weight row
-    const int64_t row = (int64_t)unit.expert * 3 * a.F + blockIdx.x * (8 * RT);
+    const int64_t row = (int64_t)expert * 3 * a.F + blockIdx.x * (8 * RT);
     Tiles tiles;
     tiles.w0 = static_cast<const char*>(a.experts) + row * pitch;
     tiles.w1 = tiles.w0 + a.F * pitch;
@@ -532,10 +556,12 @@ __global__ __launch_bounds__(kThreads, 3) void moe_up_kernel(MoeArgs a) {
     tiles.pitch = pitch;
     tiles.next = 8 * pitch;
     const int lines = (a.d + P::kLine - 1) / P::kLine, l0 = wv * lines / kWaves, l1 = (wv + 1) * lines / kWaves;
-    if (n <= 8)
-        up_product<FORMAT, RT, 1>(a, unit, n, tiles, l0, l1, lines, lds[wv], red[wv]);
+    if constexpr (ONE)
+        up_product<FORMAT, RT, 1>(a, nullptr, 1, tiles, l0, l1, lines, lds[wv], red[wv]);
+    else if (n <= 8)
+        up_product<FORMAT, RT, 1>(a, unit->token, n, tiles, l0, l1, lines, lds[wv], red[wv]);
     else
-        up_product<FORMAT, RT, 2>(a, unit, n, tiles, l0, l1, lines, lds[wv], red[wv]);
+        up_product<FORMAT, RT, 2>(a, unit->token, n, tiles, l0, l1, lines, lds[wv], red[wv]);
     __syncthreads();
     // lane (c, q) of a product holds rows 4 q .. of column c: q = 0, 1 W_gate's, 2, 3 W_up's
     if (wv >= RT || lane >= 32 || r >= n) return;
@@ -545,7 +571,7 @@ __global__ __launch_bounds__(kThreads, 3) void moe_up_kernel(MoeArgs a) {
         g += red[k][wv][lane];
         u += red[k][wv][lane + 32];
     }
-    const int64_t at = unit.row + r;
+    const int64_t at = row0 + r;
     const int f = (blockIdx.x * RT + wv) * 8 + (lane >> 4) * 4;
     f32x4 v;
 #pragma unroll
@@ -609,6 +635,65 @@ __device__ __forceinline__ void down_product(const MoeArgs& a, int row, int n, c
         for (int g = 0; g < G; ++g) red[t][g][lane] = acc[t][g];
 }
 
+// The weights of W_down's rows row0 .. of an expert.
+template <int FORMAT>
+__device__ __forceinline__ Tiles down_tiles(const MoeArgs& a, int expert, int row0) {
+    using P = Format<FORMAT>;
+    const int64_t pitch = (int64_t)a.F * 128 / P::kLine;
+    const int64_t before = ((int64_t)expert * 3 + 2) * a.F * ((int64_t)a.d * 128 / P::kLine) + row0 * pitch;
+    Tiles t;
+    t.w0 = static_cast<const char*>(a.experts) + before;
+    t.w1 = t.w0 + 8 * pitch;
+    t.s0 = FORMAT == kMoeMx8 ? a.scales + before / 32 : nullptr;
+    t.s1 = FORMAT == kMoeMx8 ? t.s0 + 8 * (pitch / 32) : nullptr;
+    t.pitch = pitch;
+    t.next = 16 * pitch;
+    return t;
+}
+
+// Down projection and gated sum of one token: a workgroup takes 16 outputs, its
+// wavefronts a part of an expert's sum each, `split` parts.
+// grid: x = d / 16
+constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64;
+template <int FORMAT>
+__global__ __launch_bounds__(kOneThreads) void moe_down_one_kernel(MoeArgs a, int split) {
+    using P = Format<FORMAT>;
+    __shared__ __align__(16) char lds[kOneWaves][kLineBytes<FORMAT, 1, 1>];
+    __shared__ __align__(16) float red[kMaxK][16];  // K split is at most 16, or K
+    __shared__ float gate[kMaxK];                   // 0 for an expert that is not selected
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lines = (a.F + P::kLine - 1) / P::kLine;
+    if (live_tokens(a) == 0) return;
+    if (threadIdx.x < a.K) gate[threadIdx.x] = a.gate[threadIdx.x];
+    for (int job = wv; job < a.K * split; job += kOneWaves) {
+        const int k = job / split, part = job % split;
+        const MoeUnit& unit = a.plan->unit[k];
+        if (unit.n == 0) {
+            if (lane < 4) *reinterpret_cast<f32x4*>(&red[job][4 * lane]) = f32x4{0.f, 0.f, 0.f, 0.f};
+            continue;
+        }
+        const char* x[1] = {static_cast<const char*>(a.act) +
+                            ((int64_t)k * P::kPlanes + min(lane >> 3, P::kPlanes - 1)) * a.F * P::kBytes + (lane & 7) * 16};
+        f32x4 acc[1][1] = {};
+        const Tiles tiles = down_tiles<FORMAT>(a, unit.expert, blockIdx.x * 16);
+        Product<FORMAT, 1, 1>{tiles, x, P::kPlanes, part * lines / split, (part + 1) * lines / split, lines, lds[wv]}.run(acc);
+        f32x4 v = acc[0][0];
+        if constexpr (P::kPlanes == 3)  // columns 0, 1, 2, the smallest first
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = (__shfl(v[j], lane + 2) + __shfl(v[j], lane + 1)) + v[j];
+        if ((lane & 15) == 0) *reinterpret_cast<f32x4*>(&red[job][4 * (lane >> 4)]) = v;
+    }
+    __syncthreads();
+    if (threadIdx.x >= 16) return;
+    float y = 0.0f;
+    for (int k = 0; k < a.K; ++k) {
+        float o = 0.0f;
+        for (int p = 0; p < split; ++p) o += red[k * split + p][threadIdx.x];
+        y += gate[k] * o;
+    }
+    a.y[blockIdx.x * 16 + threadIdx.x] = y;
+}
+
 // Down projection: the workgroup's wavefronts take RT tiles of 16 rows and a part
 // of the sum each, `split` parts.
 // grid: x = d / 16 / (RT kWaves / split) rounded up, y = units
@@ -625,15 +710,7 @@ __global__ __launch_bounds__(kThreads, 3) void moe_down_kernel(MoeArgs a, int sp
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
     const int part = wv % split, tile0 = (blockIdx.x * (kWaves / split) + wv / split) * RT, all = a.d / 16;
     if (tile0 < all) {  // d / 16 is a multiple of RT
-        Tiles tiles;
-        const int64_t pitch = (int64_t)a.F * 128 / P::kLine, before = ((int64_t)unit.expert * 3 + 2) * a.F * ((int64_t)a.d * 128 / P::kLine) +
-                                                                      tile0 * 16 * pitch;
-        tiles.w0 = static_cast<const char*>(a.experts) + before;
-        tiles.w1 = tiles.w0 + 8 * pitch;
-        tiles.s0 = FORMAT == kMoeMx8 ? a.scales + before / 32 : nullptr;
-        tiles.s1 = FORMAT == kMoeMx8 ? tiles.s0 + 8 * (pitch / 32) : nullptr;
-        tiles.pitch = pitch;
-        tiles.next = 16 * pitch;
+        const Tiles tiles = down_tiles<FORMAT>(a, unit.expert, tile0 * 16);
         const int lines = (a.F + P::kLine - 1) / P::kLine, l0 = part * lines / split, l1 = (part + 1) * lines / split;
         const int columns = P::kPlanes * n;
         if (columns <= 8)
@@ -670,18 +747,25 @@ void launch_route(const MoeArgs& a, hipStream_t st) {
         launch_kernel(moe_logits_kernel<BF16, 1>, dim3(a.N, 1), dim3(kThreads), st, Timing{}, a);
     else
         launch_kernel(moe_logits_kernel<BF16, 8>, dim3(a.N, (a.T + 7) / 8), dim3(kThreads), st, Timing{}, a);
-    launch_kernel(moe_plan_kernel, dim3(1), dim3(kPlanThreads), st, Timing{}, a);
 }
 
 template <int FORMAT>
 void launch_experts(const MoeArgs& a, hipStream_t st) {
     const int rows = a.T * a.K, units = moe_max_units(rows, a.N);
     const int lines = (a.F + Format<FORMAT>::kLine - 1) / Format<FORMAT>::kLine;
+    if (a.T == 1) {
+        launch_kernel(moe_up_kernel<FORMAT, 1, true>, dim3(a.F / 8, a.K), dim3(kThreads), st, Timing{}, a);
+        int split = 1;
+        while (2 * split * a.K <= kOneWaves && 2 * split <= lines) split *= 2;
+        launch_kernel(moe_down_one_kernel<FORMAT>, dim3(a.d / 16), dim3(kOneThreads), st, Timing{}, a, split);
+        return;
+    }
+    launch_kernel(moe_plan_kernel, dim3(1), dim3(kPlanThreads), st, Timing{}, a);
     const bool few = (int64_t)(a.F / 16) * units < 1024;
     if (few)
-        launch_kernel(moe_up_kernel<FORMAT, 1>, dim3(a.F / 8, units), dim3(kThreads), st, Timing{}, a);
+        launch_kernel(moe_up_kernel<FORMAT, 1, false>, dim3(a.F / 8, units), dim3(kThreads), st, Timing{}, a);
     else
-        launch_kernel(moe_up_kernel<FORMAT, 2>, dim3(a.F / 16, units), dim3(kThreads), st, Timing{}, a);
+        launch_kernel(moe_up_kernel<FORMAT, 2, false>, dim3(a.F / 16, units), dim3(kThreads), st, Timing{}, a);
     // parts of the down sum: four lines at least, more parts where the tiles alone
     // do not fill the device
     int split = lines >= 32 ? 4 : lines >= 16 ? 2 : 1;

@@ -179,3 +179,16 @@ def test_binding_refuses_tensors_that_do_not_fit():
     for args in ((r.half(), q, s), (r, q[:3], s), (r, q, s[:, :1]), (r, q.float(), s), (r, q, s)):
         with pytest.raises(B.CmoeError):
             B.cmoe_quantize(*args)
+
+
+def test_packed_arguments_have_the_structures_layout():
+    """The binding packs calls as bytes: field for field what the structures hold."""
+    v = list(range(1, 6)) + [(1 << 40) + i for i in range(14)]
+    v[4] = 0.5
+    n = B.cmoe_norm.from_buffer_copy(B._NORM.pack(*v))
+    assert ctypes.sizeof(B.cmoe_norm) == B._NORM.size
+    assert [getattr(n, f) for f, _ in B.cmoe_norm._fields_] == v
+    v = [3, 4] + [(1 << 40) + i for i in range(11)]
+    c = B.cmoe_moe_call.from_buffer_copy(B._CALL.pack(*v))
+    assert ctypes.sizeof(B.cmoe_moe_call) == B._CALL.size
+    assert [getattr(c, f) for f, _ in B.cmoe_moe_call._fields_] == v
