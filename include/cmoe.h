@@ -428,8 +428,8 @@ cmoe_status cmoe_moe_query(const cmoe_moe_config* cfg, size_t* workspace_bytes);
 cmoe_status cmoe_moe_init(const cmoe_moe_config* cfg, const cmoe_moe_weights* w, void* workspace, void* stream,
                           cmoe_moe** out);
 
-/* One layer's call.  Strides count values (h8 and h8_scale: bytes); rows of h
- * and y are 16-byte aligned; outputs overlap no input and no other output. */
+/* One layer's call.  Strides count values (h8 and h8_scale: bytes); rows of h,
+ * h8 and y are 16-byte aligned; outputs overlap no input and no other output. */
 typedef struct {
     int32_t layer;
     int32_t T;                /* rows, 0 .. the configuration's T                   */
@@ -443,8 +443,8 @@ typedef struct {
     float* y;                 /* fp32 output rows                                   */
     int64_t y_stride;
     const int32_t* n_tokens;  /* device: rows behind *n_tokens (held to [0, T]) are
-                                 padding, not read and left as they were in every
-                                 output; NULL: all rows are tokens                  */
+                                 padding: their values do not matter, and in every
+                                 output they are left as they were; NULL: none      */
     int32_t* selected;        /* [T][K] selected experts in descending logit, or NULL */
     float* gates;             /* [T][K] their weights, or NULL                      */
 } cmoe_moe_call;

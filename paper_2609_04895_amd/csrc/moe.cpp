@@ -334,6 +334,7 @@ cmoe_status cmoe_moe_layer(cmoe_moe* m, const cmoe_moe_call* c) {
     if (a8 && (!c->h8 || !c->h8_scale)) return fail(CMOE_ERR_INVALID_ARG, "h8 and h8_scale are required with 8-bit activations");
     if (a8 && (c->h8_stride < g.d || c->h8_scale_stride < g.d / 32))
         return fail(CMOE_ERR_INVALID_ARG, "a row stride of h8 or h8_scale is less than the row");
+    if (a8 && (!aligned_to(c->h8, 16) || c->h8_stride % 16)) return fail(CMOE_ERR_UNSUPPORTED, "rows of h8 must be 16-byte aligned");
     if (!a8 && (c->h8 || c->h8_scale)) return fail(CMOE_ERR_INVALID_ARG, "h8 is given, but the configuration's activations are not 8-bit");
     if (static_cast<const void*>(c->y) == c->h) return fail(CMOE_ERR_INVALID_ARG, "y has the place of h");
     return run_layer(m, c, c->h, c->h_stride, c->h8, c->h8_stride, c->h8_scale, c->h8_scale_stride);

@@ -53,23 +53,24 @@ __device__ inline void load8(const void* p, int64_t i, float* v) {
     }
 }
 
-// Sums of v[0 .. TG) over the wavefront: lane l gets that of v[l % TG].  While
-// there are several values, half of them go to the partner lane, so that TG
-// values take TG - 1 + log2(64 / TG) exchanges.
-template <int TG>
-__device__ inline double wave_sums(double* v, int lane) {
+// Sums of v[0 .. N) over the wavefront: lane l gets that of v[l % N].  While there
+// are several values, half of them go to the partner lane, so that N values take
+// N - 1 + log2(64 / N) exchanges.  ALL: the N of the first call.
+template <int N, int ALL = N>
+__device__ __forceinline__ double wave_sums(const double (&v)[N], int lane) {
+    if constexpr (N == 1) {
+        double s = v[0];
 #pragma unroll
-    for (int n = TG / 2; n >= 1; n /= 2) {
+        for (int m = ALL; m < 64; m *= 2) s += __shfl_xor(s, m);
+        return s;
+    } else {
+        constexpr int n = N / 2;
         const bool up = lane & n;
+        double h[n];
 #pragma unroll
-        for (int i = 0; i < n; ++i) {
-            const double give = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
-            v[i] = keep + __shfl_xor(give, n);
-        }
+        for (int i = 0; i < n; ++i) h[i] = (up ? v[i + n] : v[i]) + __shfl_xor(up ? v[i] : v[i + n], n);
+        return wave_sums<n, ALL>(h, lane);
     }
-#pragma unroll
-    for (int m = TG; m < 64; m *= 2) v[0] += __shfl_xor(v[0], m);
-    return v[0];
 }
 
 // Largest of 64 unsigned numbers, uniform.
@@ -221,42 +222,70 @@ __global__ __launch_bounds__(kPlanThreads) void moe_plan_kernel(MoeArgs a) {
 
 // Logits, summed in fp64 and rounded to fp32 once after the bias, as the cache
 // step's router does: they decide the selection.  A bias of -inf takes its expert
-// out whatever the sum is.
-// grid: x = experts, y = groups of TG tokens; the wavefronts share the sum.
-template <bool BF16, int TG>
+// out whatever the sum is.  Widening a value to fp64 takes as long as four
+// products: EG experts share each of a token's.
+// grid: x = groups of EG experts, y = groups of TG tokens; the wavefronts share the sum.
+template <bool BF16, int EG, int TG>
 __global__ __launch_bounds__(kThreads) void moe_logits_kernel(MoeArgs a) {
-    __shared__ double red[kWaves][TG];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, t0 = blockIdx.y * TG;
-    const int e = blockIdx.x, rows = min(a.T - t0, TG);
-    double acc[TG] = {};
+    __shared__ double red[kWaves][EG * TG];
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, t0 = blockIdx.y * TG, e0 = blockIdx.x * EG;
+    const int rows = min(a.T - t0, TG);
+    double acc[EG * TG] = {};
     for (int i = threadIdx.x * 8; i < a.d; i += kThreads * 8) {
-        float w[8], x[TG][8];
-        load8<BF16>(a.w_router, (int64_t)e * a.d + i, w);
+        float w[EG][8], x[TG][8];
+#pragma unroll
+        for (int e = 0; e < EG; ++e) load8<BF16>(a.w_router, (int64_t)min(e0 + e, a.N - 1) * a.d + i, w[e]);
 #pragma unroll
         for (int t = 0; t < TG; ++t) load8<BF16>(a.h, (int64_t)(t0 + min(t, rows - 1)) * a.h_stride + i, x[t]);
         __builtin_amdgcn_sched_barrier(0);  // every load before the first use
 #pragma unroll
-        for (int t = 0; t < TG; ++t)
+        for (int j = 0; j < 8; ++j) {
+            double v[EG];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) acc[t] = __builtin_fma((double)w[j], (double)x[t][j], acc[t]);
+            for (int e = 0; e < EG; ++e) v[e] = (double)w[e][j];
+#pragma unroll
+            for (int t = 0; t < TG; ++t) {
+                const double u = (double)x[t][j];
+#pragma unroll
+                for (int e = 0; e < EG; ++e) acc[e * TG + t] = __builtin_fma(v[e], u, acc[e * TG + t]);
+            }
+        }
     }
-    const double part = wave_sums<TG>(acc, lane);
-    if (lane < TG) red[wv][lane] = part;
+    const double part = wave_sums(acc, lane);
+    if (lane < EG * TG) red[wv][lane] = part;
     __syncthreads();
-    if (threadIdx.x < rows) {
+    if (threadIdx.x < EG * TG) {
+        const int e = e0 + lane / TG, t = lane % TG;
         double s = red[0][lane];
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) s += red[w][lane];
-        const float b = a.bias ? a.bias[e] : 0.0f;
-        a.z[(int64_t)(t0 + lane) * a.N + e] = b == -INFINITY ? -INFINITY : (float)(s + (double)b);
+        if (e < a.N && t < rows) {
+            const float b = a.bias ? a.bias[e] : 0.0f;
+            a.z[(int64_t)(t0 + t) * a.N + e] = b == -INFINITY ? -INFINITY : (float)(s + (double)b);
+        }
     }
-    if (a.h8)  // the experts' 8-bit input as bf16, in which every value is exact
+    if (a.h8)  // the experts' 8-bit input as bf16, in which every value is exact; 16 values per thread
         for (int64_t t = t0 + blockIdx.x; t < t0 + rows; t += gridDim.x)
-            for (int i = threadIdx.x; i < a.d; i += kThreads) {
-                const uint32_t byte = a.h8_scale[t * a.h8_scale_stride + i / 32];
-                const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a.h8[t * a.h8_stride + i],
-                                                                           __uint_as_float(byte << 23), false);
-                reinterpret_cast<__bf16*>(a.x)[t * a.d + i] = byte == 255 ? (__bf16)NAN : v[0];
+            for (int i = threadIdx.x; i < a.d / 16; i += kThreads) {
+                const uint32_t byte = a.h8_scale[t * a.h8_scale_stride + i / 2];
+                const u32x4 q = *reinterpret_cast<const u32x4*>(a.h8 + t * a.h8_stride + 16 * i);
+                const float s = __uint_as_float(byte << 23);
+                bf16x8 v[2];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[j], s, false);
+                    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q[j], s, true);
+                    v[j / 2][4 * (j % 2)] = lo[0];
+                    v[j / 2][4 * (j % 2) + 1] = lo[1];
+                    v[j / 2][4 * (j % 2) + 2] = hi[0];
+                    v[j / 2][4 * (j % 2) + 3] = hi[1];
+                }
+                bf16x8* to = reinterpret_cast<bf16x8*>(a.x + t * a.d + 16 * i);
+                if (byte == 255)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) v[j / 8][j % 8] = (__bf16)NAN;
+                to[0] = v[0];
+                to[1] = v[1];
             }
 }
 
@@ -344,18 +373,20 @@ template <int FORMAT, int NB>
 constexpr int kHeld = NB <= 2 ? Format<FORMAT>::kParts : 1;
 
 // Bytes of LDS that a line takes with its columns.
-template <int FORMAT, int RT, int NB>
-constexpr int kLineBytes = RT * 2048 + NB * kHeld<FORMAT, NB> * 1024;
+template <int FORMAT, int RT, int NB, bool HALF = false>
+constexpr int kLineBytes = RT * (HALF ? 1024 : 2048) + NB * kHeld<FORMAT, NB> * 1024;
 
-template <int FORMAT, int RT, int NB>
+// HALF: rows 8 .. 15 of the tiles do not exist, and what the product has in their
+// places is dropped.
+template <int FORMAT, int RT, int NB, bool HALF = false>
 struct Product {
     using P = Format<FORMAT>;
     static constexpr int G = (NB + 1) / 2;  // groups of 16 columns
     // lines in flight: 8 KB of weights where the columns leave the registers for it
-    static constexpr int CH = std::max(1, std::min(4 / RT, 8 / (NB * kHeld<FORMAT, NB>)));
+    static constexpr int CH = std::max(1, std::min((HALF ? 8 : 4) / RT, 8 / (NB * kHeld<FORMAT, NB>)));
     static constexpr int kParts = kHeld<FORMAT, NB>;
     struct Line {
-        u32x4 w[RT][2], x[NB][kParts];
+        u32x4 w[RT][HALF ? 1 : 2], x[NB][kParts];
     };
 
     const Tiles& tiles;
@@ -374,7 +405,7 @@ struct Product {
         for (int t = 0; t < RT; ++t) {
             // weights are read once: nontemporal
             v.w[t][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tiles.w0 + t * tiles.next + at));
-            v.w[t][1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tiles.w1 + t * tiles.next + at));
+            if (!HALF) v.w[t][HALF ? 0 : 1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tiles.w1 + t * tiles.next + at));
         }
     }
     // part k of the columns
@@ -388,7 +419,7 @@ struct Product {
     // batch of CH lines from l: the lanes of a row's neighbouring lines share a lookup
     __device__ __forceinline__ uint32_t load_scales(int l) const {
         if constexpr (FORMAT != kMoeMx8) return 0;
-        static_assert(CH * RT <= 4, "four pairs at most");
+        static_assert(FORMAT != kMoeMx8 || (CH * RT <= 4 && !HALF), "four pairs of whole tiles at most");
         const int t = min((lane & 3) / CH, RT - 1), at = min(l + (lane & 3) % CH, l1 - 1);
         const uint8_t* p = (lane < 32 ? tiles.s0 : tiles.s1) + ((lane >> 2) & 7) * (tiles.pitch / 32) + t * (tiles.next / 32) + 4 * at;
         if (!ragged) return *reinterpret_cast<const uint32_t*>(p);
@@ -400,11 +431,12 @@ struct Product {
     // line `next` if there is one (a wavefront's LDS accesses stay in order).
     __device__ __forceinline__ void step(Line& v, int l, int i, uint32_t scales, int next, f32x4 (&acc)[RT][G]) const {
         char* to = lds + i8 * 128 + (p8 ^ i8) * 16;
-        const char *row = lds + (r >> 3) * 1024 + (r & 7) * 128, *column = lds + RT * 2048;
+        constexpr int kColumns = RT * (HALF ? 1024 : 2048);  // their place behind the weights
+        const char *row = lds + (HALF ? 0 : r >> 3) * 1024 + (r & 7) * 128, *column = lds + kColumns;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             *reinterpret_cast<u32x4*>(to + t * 2048) = v.w[t][0];
-            *reinterpret_cast<u32x4*>(to + t * 2048 + 1024) = v.w[t][1];
+            if (!HALF) *reinterpret_cast<u32x4*>(to + t * 2048 + 1024) = v.w[t][HALF ? 0 : 1];
         }
         uint32_t four[RT] = {};
         if constexpr (FORMAT == kMoeMx8)
@@ -417,7 +449,7 @@ struct Product {
 #pragma unroll
             for (int k = 0; k < kParts; ++k)
 #pragma unroll
-                for (int j = 0; j < NB; ++j) *reinterpret_cast<u32x4*>(to + RT * 2048 + (j * kParts + k) * 1024) = v.x[j][k];
+                for (int j = 0; j < NB; ++j) *reinterpret_cast<u32x4*>(to + kColumns + (j * kParts + k) * 1024) = v.x[j][k];
             if (k0 == 0 && next >= 0) load_weights(v, next);
             if (kAtOnce == 2) {
                 if (next >= 0)
@@ -651,47 +683,57 @@ __device__ __forceinline__ Tiles down_tiles(const MoeArgs& a, int expert, int ro
     return t;
 }
 
-// Down projection and gated sum of one token: a workgroup takes 16 outputs, its
-// wavefronts a part of an expert's sum each, `split` parts.
-// grid: x = d / 16
-constexpr int kOneThreads = 1024, kOneWaves = kOneThreads / 64;
+// Down projection and gated sum of one token: a workgroup takes a tile of outputs,
+// its wavefronts a part of an expert's sum each, `split` parts.  Half tiles, which
+// give all CUs a workgroup at d = 2048, for weights of 16 and 32 bits (2048 x 768
+// bf16, eight experts: 8.5 us against 9.8 with whole ones), whole tiles for 8-bit
+// weights, of which half tiles put too few bytes in flight (2880 x 2880, four
+// experts: 14.3 us against 16.6).
+// grid: x = d / kTile
 template <int FORMAT>
-__global__ __launch_bounds__(kOneThreads) void moe_down_one_kernel(MoeArgs a, int split) {
+struct One {
+    static constexpr bool kHalf = FORMAT != kMoeMx8;
+    static constexpr int kTile = kHalf ? 8 : 16, kThreads = kHalf ? 512 : 1024, kWaves = kThreads / 64;
+};
+
+template <int FORMAT>
+__global__ __launch_bounds__(One<FORMAT>::kThreads) void moe_down_one_kernel(MoeArgs a, int split) {
     using P = Format<FORMAT>;
-    __shared__ __align__(16) char lds[kOneWaves][kLineBytes<FORMAT, 1, 1>];
-    __shared__ __align__(16) float red[kMaxK][16];  // K split is at most 16, or K
-    __shared__ float gate[kMaxK];                   // 0 for an expert that is not selected
+    using O = One<FORMAT>;
+    __shared__ __align__(16) char lds[O::kWaves][kLineBytes<FORMAT, 1, 1, O::kHalf>];
+    __shared__ __align__(16) float red[kMaxK][O::kTile];  // K split is at most kWaves, or K
+    __shared__ float gate[kMaxK];                         // 0 for an expert that is not selected
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lines = (a.F + P::kLine - 1) / P::kLine;
     if (live_tokens(a) == 0) return;
     if (threadIdx.x < a.K) gate[threadIdx.x] = a.gate[threadIdx.x];
-    for (int job = wv; job < a.K * split; job += kOneWaves) {
+    for (int job = wv; job < a.K * split; job += O::kWaves) {
         const int k = job / split, part = job % split;
         const MoeUnit& unit = a.plan->unit[k];
-        if (unit.n == 0) {
-            if (lane < 4) *reinterpret_cast<f32x4*>(&red[job][4 * lane]) = f32x4{0.f, 0.f, 0.f, 0.f};
-            continue;
-        }
-        const char* x[1] = {static_cast<const char*>(a.act) +
-                            ((int64_t)k * P::kPlanes + min(lane >> 3, P::kPlanes - 1)) * a.F * P::kBytes + (lane & 7) * 16};
-        f32x4 acc[1][1] = {};
-        const Tiles tiles = down_tiles<FORMAT>(a, unit.expert, blockIdx.x * 16);
-        Product<FORMAT, 1, 1>{tiles, x, P::kPlanes, part * lines / split, (part + 1) * lines / split, lines, lds[wv]}.run(acc);
-        f32x4 v = acc[0][0];
-        if constexpr (P::kPlanes == 3)  // columns 0, 1, 2, the smallest first
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (unit.n != 0) {
+            const char* x[1] = {static_cast<const char*>(a.act) +
+                                ((int64_t)k * P::kPlanes + min(lane >> 3, P::kPlanes - 1)) * a.F * P::kBytes + (lane & 7) * 16};
+            f32x4 acc[1][1] = {};
+            const Tiles tiles = down_tiles<FORMAT>(a, unit.expert, blockIdx.x * O::kTile);
+            Product<FORMAT, 1, 1, O::kHalf>{tiles, x, P::kPlanes, part * lines / split, (part + 1) * lines / split, lines, lds[wv]}.run(acc);
+            v = acc[0][0];
+            if constexpr (P::kPlanes == 3)  // columns 0, 1, 2, the smallest first
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = (__shfl(v[j], lane + 2) + __shfl(v[j], lane + 1)) + v[j];
-        if ((lane & 15) == 0) *reinterpret_cast<f32x4*>(&red[job][4 * (lane >> 4)]) = v;
+                for (int j = 0; j < 4; ++j) v[j] = (__shfl(v[j], lane + 2) + __shfl(v[j], lane + 1)) + v[j];
+        }
+        const int i = 4 * (lane >> 4);
+        if ((lane & 15) == 0 && i < O::kTile) *reinterpret_cast<f32x4*>(&red[job][i]) = v;
     }
     __syncthreads();
-    if (threadIdx.x >= 16) return;
+    if (threadIdx.x >= O::kTile) return;
     float y = 0.0f;
     for (int k = 0; k < a.K; ++k) {
         float o = 0.0f;
         for (int p = 0; p < split; ++p) o += red[k * split + p][threadIdx.x];
         y += gate[k] * o;
     }
-    a.y[blockIdx.x * 16 + threadIdx.x] = y;
+    a.y[blockIdx.x * O::kTile + threadIdx.x] = y;
 }
 
 // Down projection: the workgroup's wavefronts take RT tiles of 16 rows and a part
@@ -743,10 +785,13 @@ __global__ __launch_bounds__(kThreads, 3) void moe_down_kernel(MoeArgs a, int sp
 
 template <bool BF16>
 void launch_route(const MoeArgs& a, hipStream_t st) {
+    const unsigned groups = (a.T + 7) / 8;
     if (a.T == 1)
-        launch_kernel(moe_logits_kernel<BF16, 1>, dim3(a.N, 1), dim3(kThreads), st, Timing{}, a);
+        launch_kernel(moe_logits_kernel<BF16, 1, 1>, dim3(a.N, 1), dim3(kThreads), st, Timing{}, a);
+    else if (a.T <= 16)
+        launch_kernel(moe_logits_kernel<BF16, 1, 8>, dim3(a.N, groups), dim3(kThreads), st, Timing{}, a);
     else
-        launch_kernel(moe_logits_kernel<BF16, 8>, dim3(a.N, (a.T + 7) / 8), dim3(kThreads), st, Timing{}, a);
+        launch_kernel(moe_logits_kernel<BF16, 4, 8>, dim3((a.N + 3) / 4, groups), dim3(kThreads), st, Timing{}, a);
 }
 
 template <int FORMAT>
@@ -756,8 +801,8 @@ void launch_experts(const MoeArgs& a, hipStream_t st) {
     if (a.T == 1) {
         launch_kernel(moe_up_kernel<FORMAT, 1, true>, dim3(a.F / 8, a.K), dim3(kThreads), st, Timing{}, a);
         int split = 1;
-        while (2 * split * a.K <= kOneWaves && 2 * split <= lines) split *= 2;
-        launch_kernel(moe_down_one_kernel<FORMAT>, dim3(a.d / 16), dim3(kOneThreads), st, Timing{}, a, split);
+        while (2 * split * a.K <= One<FORMAT>::kWaves && 2 * split <= lines) split *= 2;
+        launch_kernel(moe_down_one_kernel<FORMAT>, dim3(a.d / One<FORMAT>::kTile), dim3(One<FORMAT>::kThreads), st, Timing{}, a, split);
         return;
     }
     launch_kernel(moe_plan_kernel, dim3(1), dim3(kPlanThreads), st, Timing{}, a);

@@ -8,8 +8,12 @@
 // launch and one trip to memory for few.
 //
 // r is rounded to the residual's type before it is squared, so that the norm is
-// that of the residual as stored.  Sums are fp32.  The 8-bit output is rounded
-// from the fp32 value of h, not from its bf16 form: one rounding.
+// that of the residual as stored.  The 8-bit output is rounded from the fp32 value
+// of h, not from its bf16 form: one rounding, and the fp32 value is nearly the
+// nearest one: squares are added eight at a time in fp32 and on from there in
+// fp64, and r w, exact for bf16, is multiplied with a factor of two fp32 numbers.
+// (With fp32 sums and r s w, values next to a border of two 8-bit numbers fell to
+// the other side one and a half to two times as often as in a plain fp32 form.)
 #include "cmoe_internal.h"
 #include "mx8.h"
 
@@ -45,7 +49,7 @@ __device__ inline void store8(void* p, int64_t i, const float* v) {
         bf16x8 r;
 #pragma unroll
         for (int j = 0; j < 8; ++j) r[j] = (__bf16)v[j];
-        *reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p) + i) = r;
+        __builtin_nontemporal_store(r, reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p) + i));
     } else {
         f32x4* q = reinterpret_cast<f32x4*>(static_cast<float*>(p) + i);
         q[0] = f32x4{v[0], v[1], v[2], v[3]};
@@ -77,7 +81,7 @@ __device__ inline void store1(void* p, int64_t i, float v) {
         static_cast<float*>(p)[i] = v;
 }
 
-__device__ inline float wave_sum(float v) {
+__device__ inline double wave_sum(double v) {
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m);
     return v;
@@ -86,18 +90,29 @@ __device__ inline float wave_sum(float v) {
 // Sum over the TPR threads of a row, in a fixed order; every thread gets it.
 // TPR > 64: red holds one partial per wavefront and the row is the workgroup's.
 template <int TPR>
-__device__ inline float row_sum(float v, float* red) {
+__device__ inline double row_sum(double v, double* red) {
     v = wave_sum(v);
     if constexpr (TPR > 64) {
         const int wv = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) red[wv] = v;
         __syncthreads();
-        v = 0.0f;
+        v = 0.0;
 #pragma unroll
         for (int w = 0; w < TPR / 64; ++w) v += red[w];
     }
     return v;
 }
+
+// 1 / sqrt(mean + eps) as the sum of two fp32 numbers.
+struct Factor {
+    float hi, lo;
+    __device__ Factor(double sum, const NormArgs& a) {
+        const double s = 1.0 / sqrt(sum / a.d + (double)a.eps);
+        hi = (float)s;
+        lo = fabsf(hi) < INFINITY ? (float)(s - (double)hi) : 0.0f;
+    }
+    __device__ float times(float v) const { return __builtin_fmaf(v, hi, v * lo); }
+};
 
 __device__ inline int live_rows(const NormArgs& a) {
     return a.n_rows ? min(max(*a.n_rows, 0), a.rows) : a.rows;
@@ -110,14 +125,14 @@ constexpr int kThreads = 256;  // threads of a workgroup with one wavefront per 
 // of 32 lie in neighbouring lanes.
 template <bool BF16, int DELTA, int TPR, int NV>
 __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(NormArgs a) {
-    __shared__ float red[TPR > 64 ? TPR / 64 : 1];
+    __shared__ double red[TPR > 64 ? TPR / 64 : 1];
     constexpr int RPG = TPR >= kThreads ? 1 : kThreads / TPR;  // rows per workgroup
     const int t = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * RPG + threadIdx.x / TPR;
     if (row >= live_rows(a)) return;  // whole wavefronts, and whole workgroups where they share a row
     const int ng = a.d / 8;
     float r[NV][8] = {};
-    float ss = 0.0f;
+    double ss = 0.0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int g = t + i * TPR;
@@ -139,12 +154,14 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(N
     for (int i = 0; i < NV; ++i) {
         const int g = t + i * TPR;
         if (g < ng) {
+            float s8 = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) ss += r[i][j] * r[i][j];
+            for (int j = 0; j < 8; ++j) s8 += r[i][j] * r[i][j];
+            ss += (double)s8;
             if (a.residual_out) store8<BF16>(a.residual_out, row * a.residual_out_stride + 8 * g, r[i]);
         }
     }
-    const float s = 1.0f / sqrtf(row_sum<TPR>(ss, red) / (float)a.d + a.eps);
+    const Factor s(row_sum<TPR>(ss, red), a);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int g = t + i * TPR;
@@ -153,7 +170,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(N
             float w[8];
             if (a.weight) load8<BF16>(a.weight, 8 * g, w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) r[i][j] = a.weight ? r[i][j] * s * w[j] : r[i][j] * s;
+            for (int j = 0; j < 8; ++j) r[i][j] = s.times(a.weight ? r[i][j] * w[j] : r[i][j]);
             if (a.h) store8<BF16>(a.h, row * a.h_stride + 8 * g, r[i]);
         }
         if (a.h8) {  // d % 32 == 0: the lanes of a block are all in or all out
@@ -176,7 +193,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(N
 // additions again.
 template <bool BF16, int DELTA>
 __global__ __launch_bounds__(kThreads) void norm_any_kernel(NormArgs a) {
-    __shared__ float red[kThreads / 64];
+    __shared__ double red[kThreads / 64];
     const int64_t row = blockIdx.x;
     if (row >= live_rows(a)) return;
     auto value = [&](int i) {
@@ -184,12 +201,12 @@ __global__ __launch_bounds__(kThreads) void norm_any_kernel(NormArgs a) {
         if constexpr (DELTA != 0) v = rounded<BF16>(v + load1<DELTA == 2>(a.delta, row * a.delta_stride + i));
         return v;
     };
-    float ss = 0.0f;
+    double ss = 0.0;
     for (int i = threadIdx.x; i < a.d; i += kThreads) {
         const float v = value(i);
-        ss += v * v;
+        ss += (double)(v * v);
     }
-    const float s = 1.0f / sqrtf(row_sum<kThreads>(ss, red) / (float)a.d + a.eps);
+    const Factor s(row_sum<kThreads>(ss, red), a);
     for (int i0 = 0; i0 < a.d; i0 += kThreads) {
         const int i = i0 + threadIdx.x;
         float v = 0.0f;
@@ -197,8 +214,7 @@ __global__ __launch_bounds__(kThreads) void norm_any_kernel(NormArgs a) {
             v = value(i);
             // every element is read for the last time by the thread that overwrites it
             if (a.residual_out) store1<BF16>(a.residual_out, row * a.residual_out_stride + i, v);
-            v *= s;
-            if (a.weight) v *= load1<BF16>(a.weight, i);
+            v = s.times(a.weight ? v * load1<BF16>(a.weight, i) : v);
             if (a.h) store1<BF16>(a.h, row * a.h_stride + i, v);
         }
         if (a.h8) {
@@ -231,6 +247,8 @@ hipError_t launch_norm_t(const NormArgs& a, bool aligned, hipStream_t st) {
             go(norm_kernel<BF16, DELTA, 64, 2>, 64);
         else if (ng <= 256)
             go(norm_kernel<BF16, DELTA, 64, 4>, 64);
+        else if (ng <= 384)
+            go(norm_kernel<BF16, DELTA, 64, 6>, 64);
         else
             go(norm_kernel<BF16, DELTA, 64, 8>, 64);
     } else if (ng <= 256)

@@ -482,6 +482,10 @@ def test_calls_that_are_refused():
     with pytest.raises(B.CmoeError) as err:
         layers.cmoe_moe_layer(0, odd, y, **eight)
     assert err.value.status == B.CMOE_ERR_UNSUPPORTED
+    q = torch.zeros((T, d + 8), dtype=torch.uint8, device="cuda")[:, 8:]
+    with pytest.raises(B.CmoeError) as err:
+        layers.cmoe_moe_layer(0, h, y, h8=q, h8_scale=eight["h8_scale"])
+    assert err.value.status == B.CMOE_ERR_UNSUPPORTED
     layers.cmoe_moe_layer(0, h[:0], y[:0], h8=eight["h8"][:0], h8_scale=eight["h8_scale"][:0])  # nothing to do
     plain = Model("bf16", 1, N, K, d, F, T, "refused too").layers()
     with pytest.raises(B.CmoeError):
