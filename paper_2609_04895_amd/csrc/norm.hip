@@ -21,20 +21,40 @@ namespace cmoe {
 
 namespace {
 
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-// Eight consecutive values, widened to fp32.
-template <bool BF16>
+// Eight consecutive values, widened to fp32.  NT: nontemporal, where there are so
+// many that the caches do not hold them until they are used again: the norm's
+// outputs from 1024 rows on (8192 rows of 2880: 51.9 us against 55.8; its inputs
+// too: 56.2), all of quantize from 2^26 values on (604 million bf16 values 301 us
+// against 311; 1.4 million fp32 values 4.5 us against 3.0).
+template <bool NT, typename V>
+__device__ inline V get(const void* p) {
+    if constexpr (NT)
+        return __builtin_nontemporal_load(static_cast<const V*>(p));
+    else
+        return *static_cast<const V*>(p);
+}
+template <bool NT, typename V>
+__device__ inline void put(void* p, V v) {
+    if constexpr (NT)
+        __builtin_nontemporal_store(v, static_cast<V*>(p));
+    else
+        *static_cast<V*>(p) = v;
+}
+
+template <bool BF16, bool NT = false>
 __device__ inline void load8(const void* p, int64_t i, float* v) {
     if constexpr (BF16) {
-        const bf16x8 r = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(p) + i);
+        const bf16x8 r = get<NT, bf16x8>(static_cast<const __bf16*>(p) + i);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = (float)r[j];
     } else {
-        const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
-        const f32x4 a = q[0], b = q[1];
+        const float* q = static_cast<const float*>(p) + i;
+        const f32x4 a = get<NT, f32x4>(q), b = get<NT, f32x4>(q + 4);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             v[j] = a[j];
@@ -43,17 +63,17 @@ __device__ inline void load8(const void* p, int64_t i, float* v) {
     }
 }
 
-template <bool BF16>
+template <bool BF16, bool NT = false>
 __device__ inline void store8(void* p, int64_t i, const float* v) {
     if constexpr (BF16) {
         bf16x8 r;
 #pragma unroll
         for (int j = 0; j < 8; ++j) r[j] = (__bf16)v[j];
-        __builtin_nontemporal_store(r, reinterpret_cast<bf16x8*>(static_cast<__bf16*>(p) + i));
+        put<NT>(static_cast<__bf16*>(p) + i, r);
     } else {
-        f32x4* q = reinterpret_cast<f32x4*>(static_cast<float*>(p) + i);
-        q[0] = f32x4{v[0], v[1], v[2], v[3]};
-        q[1] = f32x4{v[4], v[5], v[6], v[7]};
+        float* q = static_cast<float*>(p) + i;
+        put<NT>(q, f32x4{v[0], v[1], v[2], v[3]});
+        put<NT>(q + 4, f32x4{v[4], v[5], v[6], v[7]});
     }
 }
 
@@ -130,6 +150,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(N
     const int t = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * RPG + threadIdx.x / TPR;
     if (row >= live_rows(a)) return;  // whole wavefronts, and whole workgroups where they share a row
+    constexpr bool NT = TPR == 64;  // the launch for many rows
     const int ng = a.d / 8;
     float r[NV][8] = {};
     double ss = 0.0;
@@ -158,7 +179,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(N
 #pragma unroll
             for (int j = 0; j < 8; ++j) s8 += r[i][j] * r[i][j];
             ss += (double)s8;
-            if (a.residual_out) store8<BF16>(a.residual_out, row * a.residual_out_stride + 8 * g, r[i]);
+            if (a.residual_out) store8<BF16, NT>(a.residual_out, row * a.residual_out_stride + 8 * g, r[i]);
         }
     }
     const Factor s(row_sum<TPR>(ss, red), a);
@@ -171,7 +192,7 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(N
             if (a.weight) load8<BF16>(a.weight, 8 * g, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) r[i][j] = s.times(a.weight ? r[i][j] * w[j] : r[i][j]);
-            if (a.h) store8<BF16>(a.h, row * a.h_stride + 8 * g, r[i]);
+            if (a.h) store8<BF16, NT>(a.h, row * a.h_stride + 8 * g, r[i]);
         }
         if (a.h8) {  // d % 32 == 0: the lanes of a block are all in or all out
             float m = 0.0f;
@@ -181,7 +202,8 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(N
             m = mx_max(m, __shfl_xor(m, 2));
             if (in) {
                 const uint32_t byte = mx_scale_byte(m);
-                *reinterpret_cast<uint2*>(a.h8 + row * a.h8_stride + 8 * g) = mx_pack8(r[i], byte);
+                const uint2 q = mx_pack8(r[i], byte);
+                put<NT>(a.h8 + row * a.h8_stride + 8 * g, u32x2{q.x, q.y});
                 if ((g & 3) == 0) a.h8_scale[row * a.h8_scale_stride + g / 4] = (uint8_t)byte;
             }
         }
@@ -264,13 +286,13 @@ hipError_t launch_norm_t(const NormArgs& a, bool aligned, hipStream_t st) {
 
 // Sixteen values per thread, half a block, 16-byte loads and stores.  unit: the
 // half block's number in its row.
-template <bool BF16>
+template <bool BF16, bool NT>
 __device__ inline void quantize16(const void* src, int64_t at, uint8_t* q, uint8_t* scale, int64_t unit, bool in) {
     float v[16] = {};
     float m = 0.0f;
     if (in) {
-        load8<BF16>(src, at, v);
-        load8<BF16>(src, at + 8, v + 8);
+        load8<BF16, NT>(src, at, v);
+        load8<BF16, NT>(src, at + 8, v + 8);
 #pragma unroll
         for (int j = 0; j < 16; ++j) m = mx_max(m, v[j]);
     }
@@ -278,16 +300,16 @@ __device__ inline void quantize16(const void* src, int64_t at, uint8_t* q, uint8
     if (!in) return;
     const uint32_t byte = mx_scale_byte(m);
     const uint2 a = mx_pack8(v, byte), b = mx_pack8(v + 8, byte);
-    *reinterpret_cast<u32x4*>(q + 16 * unit) = u32x4{a.x, a.y, b.x, b.y};
+    put<NT>(q + 16 * unit, u32x4{a.x, a.y, b.x, b.y});
     if ((unit & 1) == 0) scale[unit / 2] = (uint8_t)byte;
 }
 
 // Rows that follow each other without gaps: one long row.
-template <bool BF16>
+template <bool BF16, bool NT>
 __global__ __launch_bounds__(kThreads) void quantize_flat_kernel(QuantizeArgs a) {
     const int64_t u = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     const bool in = u < a.rows * (a.cols / 16);
-    quantize16<BF16>(a.src, 16 * u, a.q, a.scale, u, in);
+    quantize16<BF16, NT>(a.src, 16 * u, a.q, a.scale, u, in);
 }
 
 // Rows apart: tpr threads (a power of two, at least 2) per row and step.
@@ -297,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(QuantizeArgs a,
     const int t = threadIdx.x % tpr, n = (int)(a.cols / 16);
     for (int u0 = 0; u0 < n; u0 += tpr) {
         const int u = u0 + t;
-        quantize16<BF16>(a.src, row * a.src_stride + (int64_t)16 * u, a.q + row * a.q_stride, a.scale + row * a.scale_stride, u,
+        quantize16<BF16, false>(a.src, row * a.src_stride + (int64_t)16 * u, a.q + row * a.q_stride, a.scale + row * a.scale_stride, u,
                          row < a.rows && u < n);
     }
 }
@@ -306,7 +328,7 @@ template <bool BF16>
 hipError_t launch_quantize_t(const QuantizeArgs& a, hipStream_t st) {
     const int64_t units = a.rows * (a.cols / 16);
     if (a.src_stride == a.cols && a.q_stride == a.cols && a.scale_stride == a.cols / kMxBlock) {
-        launch_kernel(quantize_flat_kernel<BF16>, dim3((unsigned)((units + kThreads - 1) / kThreads)), dim3(kThreads), st,
+        launch_kernel(units >= 1 << 22 ? quantize_flat_kernel<BF16, true> : quantize_flat_kernel<BF16, false>, dim3((unsigned)((units + kThreads - 1) / kThreads)), dim3(kThreads), st,
                       Timing{}, a);
     } else {
         int tpr = 2;
