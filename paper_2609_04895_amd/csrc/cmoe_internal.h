@@ -211,8 +211,9 @@ enum MoeFormat { kMoeF32 = 0, kMoeBf16 = 1, kMoeMx8 = 2 };  // of the expert wei
 struct MoeUnit {
     int32_t expert;
     int32_t n;                      // tokens, 0 past the last unit
-    int32_t row;                    // row of the first one in act and out
+    int32_t row;                    // row of the first one in act
     uint8_t token[kMoeUnitTokens];  // the last one repeated past n
+    uint16_t slot[kMoeUnitTokens];  // (token, place of the expert in its selection): row of out
 };
 
 // The experts' work of a call.
@@ -247,11 +248,10 @@ struct MoeArgs {
     // workspace
     MoePlan* plan;
     float* z;               // [T][N]   logits
-    float* gate;            // [T][K]
-    int32_t* row_of;        // [T][K]   row of a token's expert in out, -1: none
+    float* gate;            // [T][K]   -1: no expert is selected here
     uint16_t* x;            // [T][d]   bf16 values of h8
-    void* act;              // SwiGLU intermediate by row: [3][F] bf16 or [F] fp32
-    float* out;             // [rows][d] expert outputs; a row is one (expert, token), in that order
+    void* act;              // SwiGLU intermediate of each (expert, token), in that order: [3][F] bf16 or [F] fp32
+    float* out;             // [T][K][d] expert outputs
 };
 hipError_t launch_moe(const MoeArgs& a, hipStream_t st);
 

@@ -134,31 +134,33 @@ __device__ inline int select_experts(const MoeArgs& a, int t, int lane, int coun
     const int e = none ? -1 : expert;
     if (lane < a.K) {
         const int64_t at = (int64_t)t * a.K + lane;
-        const float g = none ? 0.0f : p / s;
-        a.gate[at] = g;
+        const float g = p / s;
+        a.gate[at] = none ? -1.0f : g;
         if (a.selected) a.selected[at] = e;
-        if (a.gates) a.gates[at] = g;
+        if (a.gates) a.gates[at] = none ? 0.0f : g;
     }
     return e;
 }
 
-// Selection of all tokens and the plan of the experts' work: units of up to 16
-// tokens of an expert, and the row of every (token, expert).  One workgroup: what
-// its wavefronts hand each other stays in LDS.
+// Selection of all tokens and the plan of the experts' work, units of up to 16
+// tokens of an expert.  One workgroup: what its wavefronts hand each other stays in
+// LDS.  Logits of rows behind the last token are there too; they are not waited
+// for a count that says so, only dropped.
 constexpr int kPlanThreads = 1024;
 __global__ __launch_bounds__(kPlanThreads) void moe_plan_kernel(MoeArgs a) {
-    __shared__ unsigned long long mask[kMaxN];  // tokens of each expert, one bit each
+    __shared__ unsigned long long mask[kMaxN];    // tokens of each expert, one bit each
+    __shared__ uint8_t place[kMaxN][kMoeTokens];  // of the expert in the token's selection
     __shared__ uint16_t first[kMaxN], unit0[kMaxN];
-    __shared__ int16_t sel[kMoeTokens * kMaxK];
     __shared__ int units;
-    const int tid = threadIdx.x, lane = tid & 63, n = live_tokens(a), all = a.T * a.K;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int n = live_tokens(a);
     if (tid < kMaxN) mask[tid] = 0;
     __syncthreads();
     for (int t = tid >> 6; t < a.T; t += kPlanThreads / 64) {
-        const int e = t < n ? select_experts(a, t, lane, a.K, true) : -1;
-        if (lane < a.K) {
-            sel[t * a.K + lane] = (int16_t)e;
-            if (e >= 0) atomicOr(&mask[e], 1ull << t);
+        const int e = select_experts(a, t, lane, a.K, t < n);
+        if (lane < a.K && e >= 0 && t < n) {
+            place[e][t] = (uint8_t)lane;
+            atomicOr(&mask[e], 1ull << t);
         }
     }
     __syncthreads();
@@ -208,16 +210,13 @@ __global__ __launch_bounds__(kPlanThreads) void moe_plan_kernel(MoeArgs a) {
                     ++r.n;
                 }
                 r.token[c] = (uint8_t)t;
+                r.slot[c] = (uint16_t)(t * a.K + place[tid][t]);
             }
             row += r.n;
             a.plan->unit[u] = r;
         }
     }
-    for (int i = tid; i < all; i += kPlanThreads) {
-        const int e = sel[i];
-        a.row_of[i] = e < 0 ? -1 : first[e] + __popcll(mask[e] & ((1ull << (i / a.K)) - 1));
-    }
-    for (int i = units + tid; i < moe_max_units(all, a.N); i += kPlanThreads) a.plan->unit[i].n = 0;
+    for (int i = units + tid; i < moe_max_units(a.T * a.K, a.N); i += kPlanThreads) a.plan->unit[i].n = 0;
 }
 
 // Logits, summed in fp64 and rounded to fp32 once after the bias, as the cache
@@ -632,14 +631,14 @@ __global__ __launch_bounds__(kThreads) void moe_sum_kernel(MoeArgs a) {
         float g[kBatch];
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-            const int i = t * a.K + min(k0 + k, a.K - 1), row = a.row_of[i];
-            g[k] = k0 + k < a.K && row >= 0 ? a.gate[i] : -1.0f;
-            o[k] = *reinterpret_cast<const f32x4*>(a.out + (int64_t)max(row, 0) * a.d + j);
+            const int i = t * a.K + min(k0 + k, a.K - 1);
+            g[k] = k0 + k < a.K ? a.gate[i] : -1.0f;
+            o[k] = *reinterpret_cast<const f32x4*>(a.out + (int64_t)i * a.d + j);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < kBatch; ++k)
-            if (!(g[k] < 0.0f)) y += g[k] * o[k];
+            if (!(g[k] < 0.0f)) y += g[k] * o[k];  // what is not selected was not written either
     }
     *reinterpret_cast<f32x4*>(a.y + (int64_t)t * a.y_stride + j) = y;
 }
@@ -702,7 +701,7 @@ __global__ __launch_bounds__(One<FORMAT>::kThreads) void moe_down_one_kernel(Moe
     using O = One<FORMAT>;
     __shared__ __align__(16) char lds[O::kWaves][kLineBytes<FORMAT, 1, 1, O::kHalf>];
     __shared__ __align__(16) float red[kMaxK][O::kTile];  // K split is at most kWaves, or K
-    __shared__ float gate[kMaxK];                         // 0 for an expert that is not selected
+    __shared__ float gate[kMaxK];                         // its product of an expert that is not selected is 0
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lines = (a.F + P::kLine - 1) / P::kLine;
     if (live_tokens(a) == 0) return;
@@ -778,7 +777,7 @@ __global__ __launch_bounds__(kThreads, 3) void moe_down_kernel(MoeArgs a, int sp
                 const int i = p * n + r;
                 for (int k = 0; k < split; ++k) v += red(wv - part + k)[t][i >> 4][16 * q + (i & 15)];
             }
-            *reinterpret_cast<f32x4*>(a.out + (int64_t)(unit.row + r) * a.d + tile * 16 + 4 * q) = v;
+            *reinterpret_cast<f32x4*>(a.out + (int64_t)unit.slot[r] * a.d + tile * 16 + 4 * q) = v;
         }
     }
 }
@@ -789,7 +788,7 @@ void launch_route(const MoeArgs& a, hipStream_t st) {
     if (a.T == 1)
         launch_kernel(moe_logits_kernel<BF16, 1, 1>, dim3(a.N, 1), dim3(kThreads), st, Timing{}, a);
     else if (a.T <= 16)
-        launch_kernel(moe_logits_kernel<BF16, 1, 8>, dim3(a.N, groups), dim3(kThreads), st, Timing{}, a);
+        launch_kernel(moe_logits_kernel<BF16, 1, 4>, dim3(a.N, (a.T + 3) / 4), dim3(kThreads), st, Timing{}, a);
     else
         launch_kernel(moe_logits_kernel<BF16, 4, 8>, dim3((a.N + 3) / 4, groups), dim3(kThreads), st, Timing{}, a);
 }
