@@ -449,14 +449,14 @@ struct Product {
             for (int k = 0; k < kParts; ++k)
 #pragma unroll
                 for (int j = 0; j < NB; ++j) *reinterpret_cast<u32x4*>(to + kColumns + (j * kParts + k) * 1024) = v.x[j][k];
+            // loads arrive in the order asked for: what this line still needs comes first
+            if (kAtOnce == 1 && k0 == 0) load_columns(v, l, 1);
             if (k0 == 0 && next >= 0) load_weights(v, next);
             if (kAtOnce == 2) {
                 if (next >= 0)
 #pragma unroll
                     for (int k = 0; k < kParts; ++k) load_columns(v, next, k);
-            } else if (k0 == 0) {
-                load_columns(v, l, 1);
-            } else if (next >= 0) {
+            } else if (k0 == 1 && next >= 0) {
                 load_columns(v, next, 0);
             }
             __builtin_amdgcn_wave_barrier();
@@ -549,7 +549,7 @@ __device__ __forceinline__ void up_product(const MoeArgs& a, const uint8_t* toke
 // launch, and one of them leaves the plan for the down projection.
 // grid: x = F / (8 RT), y = units
 template <int FORMAT, int RT, bool ONE>
-__global__ __launch_bounds__(kThreads, 3) void moe_up_kernel(MoeArgs a) {
+__global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeArgs a) {
     using P = Format<FORMAT>;
     __shared__ __align__(16) char lds[kWaves][kLineBytes<FORMAT, RT, ONE ? 1 : 2>];
     __shared__ f32x4 red[kWaves][RT][64];
