@@ -303,6 +303,66 @@ def overlap_study(w, warmup, steps):
     return out
 
 
+def moe_blocks(w, tokens, warmup, steps, mx8):
+    """The workload's layers without caches, one after the other on a residual
+    stream: cmoe_moe_block per layer (its output the next one's delta), then
+    cmoe_add_norm; `tokens` tokens a pass, weights in the workload's type or, with
+    mx8, in 8 bits (cmoe_quantize).  A pass is one decode step of a small batch
+    through the L layers, captured into a HIP graph."""
+    import torch
+
+    import synth
+    from paper_2609_04895_amd import cmoe as B
+    inputs = synth.device_inputs(w, T=1)
+    experts, scales = B.quantize_experts(inputs["pool"].view(w.L, w.N, -1)) if mx8 else (inputs["pool"], None)
+    if mx8:
+        del inputs["pool"]
+    fmt = B.CMOE_FORMAT_MX8 if mx8 else B.CMOE_FORMAT_DTYPE
+    dt = torch.bfloat16 if w.dtype == synth.DTYPE_BF16 else torch.float32
+    cfg = B.make_moe_config(w.L, w.N, w.K, w.d, w.F, tokens, B.CMOE_BF16 if w.dtype == synth.DTYPE_BF16 else B.CMOE_F32, fmt, fmt)
+    stream = torch.cuda.Stream()
+    layers = B.MoeLayers(cfg, inputs["wR"], inputs["bias"], experts, scales, stream=stream)
+    gen = torch.Generator(device="cuda").manual_seed(w.seed)
+    start = torch.empty((tokens, w.d), dtype=dt, device="cuda").normal_(generator=gen)
+    residual, h = torch.empty_like(start), torch.empty_like(start)
+    y = [torch.empty((tokens, w.d), dtype=torch.float32, device="cuda") for _ in range(2)]
+    selected = torch.empty((w.L, tokens, w.K), dtype=torch.int32, device="cuda")
+
+    def step():
+        residual.copy_(start)
+        for l in range(w.L):
+            layers.cmoe_moe_block(l, residual, y[(l + 1) % 2] if l else None, y[l % 2], residual_out=residual if l else None,
+                                  selected=selected[l])
+        B.cmoe_add_norm(residual, y[(w.L + 1) % 2], None, 1e-6, residual_out=residual, h=h)
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        step()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    with torch.cuda.stream(stream):
+        for _ in range(warmup):
+            graph.replay()
+        e0.record()
+        for _ in range(steps):
+            graph.replay()
+        e1.record()
+    torch.cuda.synchronize()
+    sec = e0.elapsed_time(e1) / 1e3 / steps
+    distinct = sum(int(torch.unique(selected[l]).numel()) for l in range(w.L))
+    expert_bytes = 3 * w.d * w.F * (1 + 1 / 32) if mx8 else w.expert_bytes
+    read = distinct * expert_bytes + w.L * w.N * w.d * w.elem_bytes
+    layers.cmoe_moe_destroy()
+    return {"metric": "MoE blocks without caches, token-layer steps/s", "value": tokens * w.L / sec, "unit": "token-layer steps/s",
+            "ms_per_step": sec * 1e3, "us_per_layer": sec * 1e6 / w.L, "steps": steps, "warmup": warmup, "data": "synthetic",
+            "hbm": {"algorithmic_bytes": read, "achieved_GBs": read / sec / 1e9, "frac": read / sec / 1e9 / HBM_PEAK_GBS},
+            "config": {"workload": describe(w), "tokens": tokens, "weights": "mx8" if mx8 else "dtype",
+                       "distinct_experts_per_layer": distinct / w.L}}
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--gpus", type=int, default=1)
@@ -331,6 +391,9 @@ def main():
     ap.add_argument("--overlap-study", action="store_true",
                     help="instead of the benchmark line: measure exposed expert-loading time per token and the "
                          "transfer-overlap model of Appendix B.3 (use with --workload qwen3_30b_s1)")
+    ap.add_argument("--moe-blocks", type=int, default=None, metavar="T",
+                    help="instead of the decode step: the layers without caches (norm, router, experts), T <= 64 tokens a pass")
+    ap.add_argument("--mx8", action="store_true", help="with --moe-blocks: 8-bit expert weights and activations")
     ap.add_argument("--calibrate-copy", action="store_true",
                     help="after the timed region, run one elementwise device copy of 1 GiB (reference "
                          "kernel for scaling rocprofv3 byte counters)")
@@ -360,6 +423,9 @@ def main():
         w = w.replace(arena_slots=args.arena_slots)
     warmup = args.warmup
     steps = args.steps if args.steps is not None else max(1, w.T - warmup)
+    if args.moe_blocks is not None:
+        print(json.dumps(moe_blocks(w, args.moe_blocks, min(warmup, 16), min(steps, 200), args.mx8)), flush=True)
+        return
     if args.overlap_study:
         print(json.dumps(overlap_study(w, warmup, min(steps, w.T - warmup))), flush=True)
         return

@@ -366,6 +366,8 @@ def _rows(t, name, dtype, shape, dev):
     are contiguous; raises on any other tensor."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
         _invalid(f"{name} must be a {list(shape)} tensor of {dtype} on the other tensors' device")
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1]
     row, col = t.stride()
     if col != 1 and shape[1] > 1:
         _invalid(f"the rows of {name} must be contiguous")
