@@ -339,7 +339,8 @@ cmoe_status cmoe_read_probe(const void* src, int64_t bytes, int32_t reps, double
  * tokens straight from the weight pool, and what stands between two layers.
  * They share the conventions above (status, cmoe_last_error, caller-owned
  * buffers and streams, no hipMalloc) and are asynchronous on their stream;
- * they may be captured into a HIP graph.  Two calls that overlap in time must
+ * they may be captured into a HIP graph.  A HIP failure is not sticky here: the
+ * calls keep nothing from one to the next.  Two calls that overlap in time must
  * not share a handle (a layer's workspace belongs to its handle; handles may
  * share weights): this holds for replayed graphs too.
  *
@@ -408,7 +409,8 @@ typedef struct {
     int32_t activations; /* cmoe_format of the experts' input                     */
 } cmoe_moe_config;
 
-/* Device pointers.  experts: the cold pool's layout, [L][N] x (W_gate[F][d],
+/* Device pointers; w_router and experts 16-byte aligned, logit_bias and
+ * expert_scales 4-byte.  experts: the cold pool's layout, [L][N] x (W_gate[F][d],
  * W_up[F][d], W_down[d][F]), in dtype or one byte a value with expert_scales
  * [L][N][3 d F / 32]; the same pool can serve a cmoe_handle. */
 typedef struct {
@@ -461,7 +463,8 @@ cmoe_status cmoe_moe_layer(cmoe_moe* hd, const cmoe_moe_call* c);
 /* cmoe_add_norm followed by the layer: h is the norm's output (and, with 8-bit
  * activations, its 8-bit output), held in the workspace.  n: rows = c->T, d and
  * dtype of the configuration; h, h8, h8_scale and n_rows NULL (c->n_tokens counts
- * for both).  c: h, h8 and h8_scale NULL. */
+ * for both).  c: h, h8 and h8_scale NULL.  y may be n->delta: the norm has read
+ * it before the layer writes. */
 cmoe_status cmoe_moe_block(cmoe_moe* hd, const cmoe_norm* n, const cmoe_moe_call* c);
 
 /* Releases the handle (not the caller's buffers).  NULL is accepted. */

@@ -53,8 +53,7 @@ constexpr int32_t kMaxRows = 1 << 21;  // of one norm: its grid stays under 2^32
 
 size_t elem(int dtype) { return dtype == CMOE_BF16 ? 2 : 4; }
 
-// What a norm needs besides its stream; live: h may be missing (the caller has
-// a place for it).
+// What a norm needs besides its stream.  outputs: one at least has to be given.
 cmoe_status check_norm(const cmoe_norm* n, bool outputs) {
     if (!n) return fail(CMOE_ERR_INVALID_ARG, "norm: arguments are NULL");
     if (n->rows < 0 || n->d < 1) return fail(CMOE_ERR_INVALID_ARG, "norm: rows must be >= 0 and d >= 1");
@@ -174,14 +173,12 @@ struct cmoe_moe {
     char* ws;
     hipStream_t stream;
     int device;
-    bool broken;
 };
 
 namespace {
 
 cmoe_status usable(cmoe_moe* m) {
     if (!m) return fail(CMOE_ERR_INVALID_ARG, "handle is NULL");
-    if (m->broken) return fail(CMOE_ERR_STATE, "handle unusable after an earlier HIP error; destroy it");
     int device = -1;
     if (hipGetDevice(&device) != hipSuccess || device != m->device) {
         (void)hipGetLastError();
@@ -227,11 +224,7 @@ cmoe_status run_layer(cmoe_moe* m, const cmoe_moe_call* c, const void* h, int64_
     a.act = m->ws + m->parts.act;
     a.out = reinterpret_cast<float*>(m->ws + m->parts.out);
     const hipError_t err = cmoe::launch_moe(a, m->stream);
-    if (err != hipSuccess) {
-        m->broken = true;
-        return hip_fail(err, "MoE layer");
-    }
-    return CMOE_OK;
+    return err == hipSuccess ? CMOE_OK : hip_fail(err, "MoE layer");
 }
 
 }  // namespace
@@ -291,8 +284,9 @@ cmoe_status cmoe_moe_init(const cmoe_moe_config* cfg, const cmoe_moe_weights* w,
     if (cfg->weights == CMOE_FORMAT_MX8 && !w->expert_scales)
         return fail(CMOE_ERR_INVALID_ARG, "expert_scales is required with 8-bit weights");
     if (!workspace || !aligned_to(workspace, 256)) return fail(CMOE_ERR_INVALID_ARG, "a workspace is required, 256-byte aligned");
-    if (!aligned_to(w->w_router, 16) || !aligned_to(w->experts, 16) || !aligned_to(w->logit_bias, 4))
-        return fail(CMOE_ERR_INVALID_ARG, "w_router and experts must be 16-byte aligned");
+    if (!aligned_to(w->w_router, 16) || !aligned_to(w->experts, 16) || !aligned_to(w->logit_bias, 4) ||
+        (cfg->weights == CMOE_FORMAT_MX8 && !aligned_to(w->expert_scales, 4)))
+        return fail(CMOE_ERR_INVALID_ARG, "w_router and experts must be 16-byte aligned, logit_bias and expert_scales 4-byte");
     int device = 0;
     if ((st = current_device(&device)) != CMOE_OK) return st;
     if ((st = check_stream(static_cast<hipStream_t>(stream), device)) != CMOE_OK) return st;
@@ -364,10 +358,7 @@ cmoe_status cmoe_moe_block(cmoe_moe* m, const cmoe_norm* n, const cmoe_moe_call*
         a.h8_scale_stride = g.d / 32;
     }
     const hipError_t e = cmoe::launch_norm(a, norm_aligned(a), m->stream);
-    if (e != hipSuccess) {
-        m->broken = true;
-        return hip_fail(e, "norm");
-    }
+    if (e != hipSuccess) return hip_fail(e, "norm");
     return run_layer(m, c, a.h, a.h_stride, a.h8, a.h8_stride, a.h8_scale, a.h8_scale_stride);
 }
 

@@ -117,9 +117,10 @@ def test_layer_matches_fp64(N, K, d, F, T, kind):
 
 
 @pytest.mark.parametrize("kind", KINDS)
-def test_masks_that_leave_few_experts_or_none(kind):
+@pytest.mark.parametrize("T", [1, 20])
+def test_masks_that_leave_few_experts_or_none(kind, T):
     """Bias -inf takes experts out, whatever their router row and weights hold."""
-    N, K, d, F, T = 12, 4, 128, 64, 20
+    N, K, d, F = 12, 4, 128, 64
     for out in (3, 10, 12):
         bias = torch.randn((1, N), generator=torch.Generator().manual_seed(out)) * 0.3
         bias[0, :out] = -math.inf
@@ -217,6 +218,50 @@ def test_rows_behind_the_last_token_are_left(kind, n):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+def test_one_token_padded_away_and_one_of_nan(kind):
+    """The single-token launches: no token leaves every output, a NaN is the token's own."""
+    N, K, d, F = 16, 3, 128, 64
+    m = Model(kind, 1, N, K, d, F, 1, f"one {kind}")
+    layers, h = m.layers(), m.hidden(1)
+    y, sel, gates = outputs(1, K, d)
+    for n in (0, 1):
+        eight, x = m.eight(h)
+        layers.cmoe_moe_layer(0, h.cuda(), y, selected=sel, gates=gates, n_tokens=torch.tensor([n], dtype=torch.int32, device="cuda"), **eight)
+        if n == 0:
+            assert (y == 7).all() and (sel == -9).all() and (gates == 9).all()
+        else:
+            check((y, sel, gates), m.expected(0, h, x), K)
+    bad = h.clone()
+    bad[0, 5] = math.nan
+    eight, _ = m.eight(bad)
+    layers.cmoe_moe_layer(0, bad.cuda(), y, selected=sel, gates=gates, **eight)
+    assert y.isnan().all() and gates.isnan().all() and sel.tolist() == [[0, 1, 2]]
+    eight, x = m.eight(h)
+    layers.cmoe_moe_layer(0, h.cuda(), y, selected=sel, gates=gates, **eight)
+    check((y, sel, gates), m.expected(0, h, x), K)
+
+
+@pytest.mark.parametrize("T", [1, 6])
+@pytest.mark.parametrize("d,F", [(192, 64), (128, 192), (256, 256)])
+def test_8_bit_blocks_of_zeros_and_of_tiny_values(T, d, F):
+    """Scale bytes 0 (zeros) and near it, beside ordinary blocks; rows that end in half a line and rows that do not."""
+    N, K = 5, 2
+    m = Model("w8", 1, N, K, d, F, T, f"tiny {T} {d} {F}")
+    pool = torch.randn((1, N, 3 * d * F), generator=m.gen) * 0.05
+    b = pool.view(1, N, -1, 32)
+    b[:, :, ::3] = 0.0
+    b[:, :, 1::7] *= 2.0 ** -100
+    b[:, 0] = 0.0
+    m.gpu["experts"], m.gpu["expert_scales"] = m.B.quantize_experts(pool.cuda())
+    m.pool, m.scales = m.gpu["experts"].cpu(), m.gpu["expert_scales"].cpu()
+    assert (m.scales == 0).any()
+    h = m.hidden(T)
+    y, sel, gates = outputs(T, K, d)
+    m.layers().cmoe_moe_layer(0, h.cuda(), y, selected=sel, gates=gates)
+    check((y, sel, gates), m.expected(0, h, h), K)
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_layers_and_rows_apart(kind):
     """Rows of [T][L][d] buffers, each layer with its own weights and bias."""
     L, N, K, d, F, T = 3, 10, 3, 192, 64, 6
@@ -291,6 +336,10 @@ def test_block_is_norm_then_layer(kind, T, with_delta):
         y3, _, _ = outputs(T, K, d)
         layers.cmoe_moe_block(l, res, delta, y3)
         assert torch.equal(y3, y)
+        if with_delta:  # y in delta's place
+            y4 = delta.clone()
+            layers.cmoe_moe_block(l, res, y4, y4)
+            assert torch.equal(y4, y)
 
 
 @pytest.mark.parametrize("n", [0, 5])
@@ -436,6 +485,48 @@ def test_handles_on_two_streams_at_once():
     torch.cuda.synchronize()
     for i in range(2):
         check(outs[i], want[i], K)
+
+
+def test_a_handle_on_another_stream_than_its_tensors():
+    """Work of the current stream, waited for by the handle's stream, and back."""
+    N, K, d, F, T = 32, 4, 256, 128, 10
+    m = Model("bf16", 1, N, K, d, F, T, "other stream")
+    st = torch.cuda.Stream()
+    layers = m.layers(stream=st)
+    for i in range(5):
+        h = m.hidden(T)
+        y, sel, gates = outputs(T, K, d)
+        hg = h.cuda() + 0  # on the current stream
+        st.wait_stream(torch.cuda.current_stream())
+        layers.cmoe_moe_layer(0, hg, y, selected=sel, gates=gates)
+        torch.cuda.current_stream().wait_stream(st)
+        check((y, sel, gates), m.expected(0, h, h), K)
+
+
+def test_concurrent_host_threads_with_a_handle_each():
+    import threading
+    N, K, d, F, T = 16, 3, 128, 64, 9
+    m = Model("f32", 1, N, K, d, F, T, "threads")
+    hs = [m.hidden(T) for _ in range(4)]
+    want = [m.expected(0, h, h) for h in hs]
+    got, streams = [None] * 4, [torch.cuda.Stream() for _ in range(4)]
+    handles, gs = [m.layers(stream=s) for s in streams], [h.cuda() for h in hs]
+    torch.cuda.synchronize()
+
+    def work(i):
+        with torch.cuda.stream(streams[i]):
+            out = outputs(T, K, d)
+            for _ in range(10):
+                handles[i].cmoe_moe_layer(0, gs[i], out[0], selected=out[1], gates=out[2])
+        got[i] = out
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for i in range(4):
+        check(got[i], want[i], K)
 
 
 @pytest.mark.parametrize("kind", KINDS)

@@ -80,6 +80,9 @@ def test_moe_init_needs_scales_with_8_bit_weights():
     cfg = moe_cfg(weights=1)
     st = B.lib().cmoe_moe_init(ctypes.byref(cfg), ctypes.byref(w), P, None, ctypes.byref(h))
     assert st == B.CMOE_ERR_INVALID_ARG and "expert_scales" in error()
+    w = B.cmoe_moe_weights(P, None, P, P + 2)  # scales are read four at a time
+    st = B.lib().cmoe_moe_init(ctypes.byref(cfg), ctypes.byref(w), P, None, ctypes.byref(h))
+    assert st == B.CMOE_ERR_INVALID_ARG and "aligned" in error()
 
 
 def test_moe_calls_without_a_handle():
