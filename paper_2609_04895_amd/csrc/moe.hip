@@ -527,7 +527,7 @@ __device__ inline void split3(float v, __bf16* p) {
 }
 
 template <int FORMAT, int RT, int NB>
-__device__ __forceinline__ void up_product(const MoeArgs& a, const uint8_t* token, int n, const Tiles& tiles, int l0, int l1, int lines,
+__device__ __forceinline__ void up_product(const MoeArgs& a, const uint8_t* token, int first, int n, const Tiles& tiles, int l0, int l1, int lines,
                                            char* lds, f32x4 (*red)[64]) {
     using P = Format<FORMAT>;
     const int lane = threadIdx.x & 63, i8 = lane >> 3;
@@ -535,7 +535,7 @@ __device__ __forceinline__ void up_product(const MoeArgs& a, const uint8_t* toke
 #pragma unroll
     for (int j = 0; j < NB; ++j)
         x[j] = (a.h8 ? reinterpret_cast<const char*>(a.x) : static_cast<const char*>(a.h)) +
-               (token ? token[8 * j + i8] : 0) * (a.h8 ? (int64_t)a.d : a.h_stride) * P::kBytes + (lane & 7) * 16;
+               (token ? token[8 * j + i8] : first) * (a.h8 ? (int64_t)a.d : a.h_stride) * P::kBytes + (lane & 7) * 16;
     f32x4 acc[RT][1] = {};
     Product<FORMAT, RT, NB>{tiles, x, n, l0, l1, lines, lds}.run(acc);
 #pragma unroll
@@ -544,31 +544,30 @@ __device__ __forceinline__ void up_product(const MoeArgs& a, const uint8_t* toke
 
 // Gate and up projections and the SwiGLU product: a tile is eight rows of W_gate
 // and the same eight of W_up; a workgroup takes RT of them, its wavefronts a
-// quarter of the sum each.  ONE: there is one token, whose k-th expert is unit k:
-// every wavefront finds its own from the logits, which takes less than the plan's
-// launch, and one of them leaves the plan for the down projection.
+// quarter of the sum each.  EACH: every (token, selected expert) is a unit of its
+// own: each wavefront finds its expert from the token's logits, which takes less
+// than the plan's launch, and one per token leaves the units for the down
+// projection.
 // grid: x = F / (8 RT), y = units
-template <int FORMAT, int RT, bool ONE>
+template <int FORMAT, int RT, bool EACH>
 __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeArgs a) {
     using P = Format<FORMAT>;
-    __shared__ __align__(16) char lds[kWaves][kLineBytes<FORMAT, RT, ONE ? 1 : 2>];
+    __shared__ __align__(16) char lds[kWaves][kLineBytes<FORMAT, RT, EACH ? 1 : 2>];
     __shared__ f32x4 red[kWaves][RT][64];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
     MoeUnit* unit = a.plan->unit + blockIdx.y;
-    int expert, n, row0;
-    if constexpr (ONE) {
-        const bool write = blockIdx.x == 0 && blockIdx.y == 0 && wv == 0;
-        if (live_tokens(a) == 0) {
-            if (write && lane < a.K) a.plan->unit[lane].n = 0;
-            return;
-        }
-        const int e = select_experts(a, 0, lane, write ? a.K : blockIdx.y + 1, write);
+    int expert, n, row0, first = 0;  // first: its token, where there is no plan
+    if constexpr (EACH) {
+        const int k = blockIdx.y % a.K;
+        first = blockIdx.y / a.K;
+        if (first >= live_tokens(a)) return;
+        const bool write = blockIdx.x == 0 && k == 0 && wv == 0;
+        const int e = select_experts(a, first, lane, write ? a.K : k + 1, write);
         if (write && lane < a.K) {
             unit[lane].expert = e;
             unit[lane].n = e >= 0;
-            unit[lane].row = lane;
         }
-        expert = __builtin_amdgcn_readlane(e, blockIdx.y);
+        expert = __builtin_amdgcn_readlane(e, k);
         n = expert >= 0;
         row0 = blockIdx.y;
     } else {
@@ -587,12 +586,12 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeArgs a) {
     tiles.pitch = pitch;
     tiles.next = 8 * pitch;
     const int lines = (a.d + P::kLine - 1) / P::kLine, l0 = wv * lines / kWaves, l1 = (wv + 1) * lines / kWaves;
-    if constexpr (ONE)
-        up_product<FORMAT, RT, 1>(a, nullptr, 1, tiles, l0, l1, lines, lds[wv], red[wv]);
+    if constexpr (EACH)
+        up_product<FORMAT, RT, 1>(a, nullptr, first, 1, tiles, l0, l1, lines, lds[wv], red[wv]);
     else if (n <= 8)
-        up_product<FORMAT, RT, 1>(a, unit->token, n, tiles, l0, l1, lines, lds[wv], red[wv]);
+        up_product<FORMAT, RT, 1>(a, unit->token, 0, n, tiles, l0, l1, lines, lds[wv], red[wv]);
     else
-        up_product<FORMAT, RT, 2>(a, unit->token, n, tiles, l0, l1, lines, lds[wv], red[wv]);
+        up_product<FORMAT, RT, 2>(a, unit->token, 0, n, tiles, l0, l1, lines, lds[wv], red[wv]);
     __syncthreads();
     // lane (c, q) of a product holds rows 4 q .. of column c: q = 0, 1 W_gate's, 2, 3 W_up's
     if (wv >= RT || lane >= 32 || r >= n) return;
@@ -682,13 +681,13 @@ __device__ __forceinline__ Tiles down_tiles(const MoeArgs& a, int expert, int ro
     return t;
 }
 
-// Down projection and gated sum of one token: a workgroup takes a tile of outputs,
+// Down projection and gated sum of a token: a workgroup takes a tile of outputs,
 // its wavefronts a part of an expert's sum each, `split` parts.  Half tiles, which
 // give all CUs a workgroup at d = 2048, for weights of 16 and 32 bits (2048 x 768
 // bf16, eight experts: 8.5 us against 9.8 with whole ones), whole tiles for 8-bit
 // weights, of which half tiles put too few bytes in flight (2880 x 2880, four
 // experts: 14.3 us against 16.6).
-// grid: x = d / kTile
+// grid: x = d / kTile, y = tokens
 template <int FORMAT>
 struct One {
     static constexpr bool kHalf = FORMAT != kMoeMx8;
@@ -704,15 +703,16 @@ __global__ __launch_bounds__(One<FORMAT>::kThreads) void moe_down_one_kernel(Moe
     __shared__ float gate[kMaxK];                         // its product of an expert that is not selected is 0
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int lines = (a.F + P::kLine - 1) / P::kLine;
-    if (live_tokens(a) == 0) return;
-    if (threadIdx.x < a.K) gate[threadIdx.x] = a.gate[threadIdx.x];
+    const int first = blockIdx.y * a.K;  // the token's first unit
+    if ((int)blockIdx.y >= live_tokens(a)) return;
+    if (threadIdx.x < a.K) gate[threadIdx.x] = a.gate[first + threadIdx.x];
     for (int job = wv; job < a.K * split; job += O::kWaves) {
         const int k = job / split, part = job % split;
-        const MoeUnit& unit = a.plan->unit[k];
+        const MoeUnit& unit = a.plan->unit[first + k];
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
         if (unit.n != 0) {
             const char* x[1] = {static_cast<const char*>(a.act) +
-                                ((int64_t)k * P::kPlanes + min(lane >> 3, P::kPlanes - 1)) * a.F * P::kBytes + (lane & 7) * 16};
+                                ((int64_t)(first + k) * P::kPlanes + min(lane >> 3, P::kPlanes - 1)) * a.F * P::kBytes + (lane & 7) * 16};
             f32x4 acc[1][1] = {};
             const Tiles tiles = down_tiles<FORMAT>(a, unit.expert, blockIdx.x * O::kTile);
             Product<FORMAT, 1, 1, O::kHalf>{tiles, x, P::kPlanes, part * lines / split, (part + 1) * lines / split, lines, lds[wv]}.run(acc);
@@ -732,7 +732,7 @@ __global__ __launch_bounds__(One<FORMAT>::kThreads) void moe_down_one_kernel(Moe
         for (int p = 0; p < split; ++p) o += red[k * split + p][threadIdx.x];
         y += gate[k] * o;
     }
-    a.y[blockIdx.x * O::kTile + threadIdx.x] = y;
+    a.y[blockIdx.y * a.y_stride + blockIdx.x * O::kTile + threadIdx.x] = y;
 }
 
 // Down projection: the workgroup's wavefronts take RT tiles of 16 rows and a part
@@ -793,15 +793,29 @@ void launch_route(const MoeArgs& a, hipStream_t st) {
         launch_kernel(moe_logits_kernel<BF16, 4, 8>, dim3((a.N + 3) / 4, groups), dim3(kThreads), st, Timing{}, a);
 }
 
+// Few tokens of many experts: hardly two of them share one, and the plan's and the
+// gated sum's launches take longer than reading a shared expert's weights twice, as
+// long as the weights are not so many that the tiles of the joint launches stream
+// them faster.  Each alone against joint, us a call (top-8 of 128, 2048 x 768): bf16,
+// 2, 3 and 4 tokens (151, 226, 302 MB) 34.8 / 39.5, 47.9 / 50.9, 59.8 / 61.5; 8 bits
+// (78, 117, 156 MB) 25.3 / 33.2, 37.9 / 37.5, 42.4 / 41.2; top-6 of 256, 1024 x 512,
+// 4 tokens 24.1 / 32.9 and 19.5 / 29.8; 4096 x 1536, bf16, 4 tokens 198 / 186.
+bool each_alone(const MoeArgs& a) {
+    const int64_t rows = (int64_t)a.T * a.K, values = rows * 3 * a.d * a.F;
+    const int64_t bytes = a.format == kMoeMx8 ? values : a.format == kMoeBf16 ? 2 * values : 4 * values;
+    return a.T == 1 || (a.T <= 4 && 4 * rows <= a.N && bytes <= (a.format == kMoeMx8 ? 96 : 256) * 1000000ll);
+}
+
 template <int FORMAT>
 void launch_experts(const MoeArgs& a, hipStream_t st) {
     const int rows = a.T * a.K, units = moe_max_units(rows, a.N);
     const int lines = (a.F + Format<FORMAT>::kLine - 1) / Format<FORMAT>::kLine;
-    if (a.T == 1) {
-        launch_kernel(moe_up_kernel<FORMAT, 1, true>, dim3(a.F / 8, a.K), dim3(kThreads), st, Timing{}, a);
+    if (each_alone(a)) {
+        launch_kernel(moe_up_kernel<FORMAT, 1, true>, dim3(a.F / 8, rows), dim3(kThreads), st, Timing{}, a);
         int split = 1;
         while (2 * split * a.K <= One<FORMAT>::kWaves && 2 * split <= lines) split *= 2;
-        launch_kernel(moe_down_one_kernel<FORMAT>, dim3(a.d / One<FORMAT>::kTile), dim3(One<FORMAT>::kThreads), st, Timing{}, a, split);
+        launch_kernel(moe_down_one_kernel<FORMAT>, dim3(a.d / One<FORMAT>::kTile, a.T), dim3(One<FORMAT>::kThreads), st, Timing{}, a,
+                      split);
         return;
     }
     launch_kernel(moe_plan_kernel, dim3(1), dim3(kPlanThreads), st, Timing{}, a);
