@@ -456,7 +456,8 @@ def quantize_experts(experts):
     L, N, n = experts.shape
     q = torch.empty((L, N, n), dtype=torch.uint8, device=experts.device)
     scale = torch.empty((L, N, n // 32), dtype=torch.uint8, device=experts.device)
-    cmoe_quantize(experts.view(L * N, n), q.view(L * N, n), scale.view(L * N, n // 32))
+    for l in range(L):  # a call takes 2^34 values, a whole model's pool has more
+        cmoe_quantize(experts[l], q[l], scale[l])
     return q, scale
 
 
