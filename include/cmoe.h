@@ -354,15 +354,15 @@ cmoe_status cmoe_read_probe(const void* src, int64_t bytes, int32_t reps, double
 /* Residual addition and root-mean-square norm of `rows` rows of d values:
  *   r = fl(residual + delta)              (residual, without a delta)
  *   h = r / sqrt(mean(r^2) + eps) * weight
- * r is rounded to dtype, stored to residual_out and normalised as stored; sums
- * are fp32; h is rounded once, to dtype (h) and to 8 bits (h8, h8_scale).
+ * r is rounded to dtype, stored to residual_out and normalised as stored; squares
+ * and sums are fp64; h is rounded once, to dtype (h) and to 8 bits (h8, h8_scale).
  * Between two layer steps delta is the y of cmoe_step or cmoe_moe_layer, and h
  * the next layer's hidden states: strides let both be rows of [S][L][d].
  * Strides count values (h8 and h8_scale: bytes) and are at least the row.
  * residual_out may be residual itself (same stride); no other output may
  * overlap an input or another output.  At least one output is given. */
 typedef struct {
-    int32_t rows, d;            /* rows <= 2^21                                    */
+    int32_t rows, d;            /* rows <= 2^21, d <= 2^24                         */
     int32_t dtype;              /* cmoe_dtype of residual, residual_out, weight, h */
     int32_t delta_dtype;        /* cmoe_dtype of delta                             */
     float eps;                  /* finite, >= 0                                    */
@@ -457,7 +457,8 @@ typedef struct {
  * (W_up,k x)), k in descending logit, with fp32 sums and an intermediate that is
  * not rounded to fewer bits.  Experts with a logit of -inf are not selected
  * (index -1, gate 0); a token that selects none gets y = 0.  A NaN logit counts
- * as the largest and makes the token's gates and y NaN. */
+ * as the largest and makes the token's gates and y NaN.  An infinity among the
+ * weights of W_down makes the outputs it reaches infinite or NaN. */
 cmoe_status cmoe_moe_layer(cmoe_moe* hd, const cmoe_moe_call* c);
 
 /* cmoe_add_norm followed by the layer: h is the norm's output (and, with 8-bit

@@ -49,7 +49,8 @@ cmoe_status current_device(int* device) {
     return hip_fail(e, "hipGetDevice");
 }
 
-constexpr int32_t kMaxRows = 1 << 21;  // of one norm: its grid stays under 2^32 threads
+constexpr int32_t kMaxRows = 1 << 21;   // of one norm: its grid stays under 2^32 threads
+constexpr int32_t kMaxWidth = 1 << 24;  // of one norm: a row is one workgroup's
 
 size_t elem(int dtype) { return dtype == CMOE_BF16 ? 2 : 4; }
 
@@ -62,6 +63,7 @@ cmoe_status check_norm(const cmoe_norm* n, bool outputs) {
         return fail(CMOE_ERR_INVALID_ARG, "norm: unknown delta dtype");
     if (!(std::isfinite(n->eps) && n->eps >= 0.0f)) return fail(CMOE_ERR_INVALID_ARG, "norm: eps must be finite and >= 0");
     if (n->rows > kMaxRows) return fail(CMOE_ERR_UNSUPPORTED, "norm: more than %d rows are not supported", kMaxRows);
+    if (n->d > kMaxWidth) return fail(CMOE_ERR_UNSUPPORTED, "norm: d > %d is not supported", kMaxWidth);
     if (!n->residual && n->rows) return fail(CMOE_ERR_INVALID_ARG, "norm: residual is required");
     if (outputs && n->rows && !n->h && !n->h8 && !n->residual_out) return fail(CMOE_ERR_INVALID_ARG, "norm: no output is given");
     if (!n->h8 != !n->h8_scale) return fail(CMOE_ERR_INVALID_ARG, "norm: h8 and h8_scale go together");

@@ -10,10 +10,13 @@
 // r is rounded to the residual's type before it is squared, so that the norm is
 // that of the residual as stored.  The 8-bit output is rounded from the fp32 value
 // of h, not from its bf16 form: one rounding, and the fp32 value is nearly the
-// nearest one: squares are added eight at a time in fp32 and on from there in
-// fp64, and r w, exact for bf16, is multiplied with a factor of two fp32 numbers.
-// (With fp32 sums and r s w, values next to a border of two 8-bit numbers fell to
-// the other side one and a half to two times as often as in a plain fp32 form.)
+// nearest one: squares are taken and added in fp64, and r w, exact for bf16, is
+// multiplied with a factor of two fp32 numbers.  (With fp32 sums and r s w, values
+// next to a border of two 8-bit numbers fell to the other side one and a half to
+// two times as often as in a plain fp32 form; and squares of values beyond 2^64 or
+// below 2^-75 leave fp32's range.)
+#include <algorithm>
+
 #include "cmoe_internal.h"
 #include "mx8.h"
 
@@ -175,10 +178,8 @@ __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(N
     for (int i = 0; i < NV; ++i) {
         const int g = t + i * TPR;
         if (g < ng) {
-            float s8 = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s8 += r[i][j] * r[i][j];
-            ss += (double)s8;
+            for (int j = 0; j < 8; ++j) ss = __builtin_fma((double)r[i][j], (double)r[i][j], ss);
             if (a.residual_out) store8<BF16, NT>(a.residual_out, row * a.residual_out_stride + 8 * g, r[i]);
         }
     }
@@ -225,8 +226,8 @@ __global__ __launch_bounds__(kThreads) void norm_any_kernel(NormArgs a) {
     };
     double ss = 0.0;
     for (int i = threadIdx.x; i < a.d; i += kThreads) {
-        const float v = value(i);
-        ss += (double)(v * v);
+        const double v = (double)value(i);
+        ss = __builtin_fma(v, v, ss);
     }
     const Factor s(row_sum<kThreads>(ss, red), a);
     for (int i0 = 0; i0 < a.d; i0 += kThreads) {
@@ -313,13 +314,14 @@ __global__ __launch_bounds__(kThreads) void quantize_flat_kernel(QuantizeArgs a)
 }
 
 // Rows apart: tpr threads (a power of two, at least 2) per row and step.
+// grid: x = rows / (kThreads / tpr) rounded up, y = workgroups that share a row
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(QuantizeArgs a, int tpr) {
     const int64_t row = (int64_t)blockIdx.x * (kThreads / tpr) + threadIdx.x / tpr;
-    const int t = threadIdx.x % tpr, n = (int)(a.cols / 16);
-    for (int u0 = 0; u0 < n; u0 += tpr) {
-        const int u = u0 + t;
-        quantize16<BF16, false>(a.src, row * a.src_stride + (int64_t)16 * u, a.q + row * a.q_stride, a.scale + row * a.scale_stride, u,
+    const int64_t t = threadIdx.x % tpr, n = a.cols / 16;
+    for (int64_t u0 = (int64_t)blockIdx.y * tpr; u0 < n; u0 += (int64_t)gridDim.y * tpr) {
+        const int64_t u = u0 + t;
+        quantize16<BF16, false>(a.src, row * a.src_stride + 16 * u, a.q + row * a.q_stride, a.scale + row * a.scale_stride, u,
                          row < a.rows && u < n);
     }
 }
@@ -327,15 +329,16 @@ __global__ __launch_bounds__(kThreads) void quantize_rows_kernel(QuantizeArgs a,
 template <bool BF16>
 hipError_t launch_quantize_t(const QuantizeArgs& a, hipStream_t st) {
     const int64_t units = a.rows * (a.cols / 16);
-    if (a.src_stride == a.cols && a.q_stride == a.cols && a.scale_stride == a.cols / kMxBlock) {
-        launch_kernel(units >= 1 << 22 ? quantize_flat_kernel<BF16, true> : quantize_flat_kernel<BF16, false>, dim3((unsigned)((units + kThreads - 1) / kThreads)), dim3(kThreads), st,
-                      Timing{}, a);
+    if (a.rows == 1 || (a.src_stride == a.cols && a.q_stride == a.cols && a.scale_stride == a.cols / kMxBlock)) {
+        launch_kernel(units >= 1 << 22 ? quantize_flat_kernel<BF16, true> : quantize_flat_kernel<BF16, false>,
+                      dim3((unsigned)((units + kThreads - 1) / kThreads)), dim3(kThreads), st, Timing{}, a);
     } else {
         int tpr = 2;
         while (tpr < kThreads && tpr < a.cols / 16) tpr *= 2;
-        const int64_t rpg = kThreads / tpr;
-        launch_kernel(quantize_rows_kernel<BF16>, dim3((unsigned)((a.rows + rpg - 1) / rpg)), dim3(kThreads), st, Timing{}, a,
-                      tpr);
+        const int64_t rpg = kThreads / tpr, groups = (a.rows + rpg - 1) / rpg, steps = (a.cols / 16 + tpr - 1) / tpr;
+        // few long rows: as many workgroups each as give the device 4096 in all
+        const int64_t share = std::max<int64_t>(1, std::min(steps, 4096 / groups));
+        launch_kernel(quantize_rows_kernel<BF16>, dim3((unsigned)groups, (unsigned)share), dim3(kThreads), st, Timing{}, a, tpr);
     }
     return hipGetLastError();
 }

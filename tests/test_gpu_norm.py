@@ -176,6 +176,19 @@ def test_norm_rows_of_special_values(d):
         check_8bit(q[row:row + 1], s[row:row + 1], h64, d)
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -110, 2.0 ** -80, 2.0 ** 70, 2.0 ** 110])
+@pytest.mark.parametrize("rows,d", [(3, 256), (1024, 256), (2, 50)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_norm_squares_outside_fp32(scale, rows, d, dtype):
+    """Values whose squares leave fp32's range, without an epsilon."""
+    from paper_2609_04895_amd import cmoe as B
+    g = torch.Generator().manual_seed(17)
+    res = rows_tensor(rows, d, dtype, g, scale)
+    h = torch.empty_like(res)
+    B.cmoe_add_norm(res, None, None, 0.0, h=h)
+    check_h(h, ref.norm(res.cpu(), None, None, 0.0)[1], d, dtype)
+
+
 def test_norm_offsets_past_32_bits():
     """Two rows 2^31 + 64 values apart."""
     from paper_2609_04895_amd import cmoe as B
@@ -215,6 +228,22 @@ def test_quantize_is_exact(rows, cols, gap, dtype):
     got = q[:, :cols].cpu().contiguous().view(torch.float8_e4m3fn).double()
     assert torch.equal(got, want)
     assert (q[:, cols:] == 9).all() and (s[:, cols // 32:] == 9).all()
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3])
+def test_quantize_few_long_rows(rows):
+    """Rows apart that are far longer than a workgroup: each as on its own."""
+    from paper_2609_04895_amd import cmoe as B
+    n, gap = (1 << 24) + 32, 4096
+    x = torch.randn((rows, n + gap), generator=torch.Generator().manual_seed(3)).to(BF16).cuda()
+    q = torch.full((rows, n + gap), 9, dtype=torch.uint8, device="cuda")
+    s = torch.full((rows, n // 32 + gap), 9, dtype=torch.uint8, device="cuda")
+    B.cmoe_quantize(x[:, :n], q[:, :n], s[:, :n // 32])
+    for r in range(rows):
+        q1, s1 = torch.empty((1, n), dtype=torch.uint8, device="cuda"), torch.empty((1, n // 32), dtype=torch.uint8, device="cuda")
+        B.cmoe_quantize(x[r:r + 1, :n].contiguous(), q1, s1)
+        assert torch.equal(q[r:r + 1, :n], q1) and torch.equal(s[r:r + 1, :n // 32], s1)
+    assert (q[:, n:] == 9).all() and (s[:, n // 32:] == 9).all()
 
 
 def test_quantize_special_blocks():

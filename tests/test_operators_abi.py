@@ -109,6 +109,8 @@ def norm(**kw):
     (dict(eps=float("nan")), B.CMOE_ERR_INVALID_ARG, "eps"),
     (dict(eps=float("inf")), B.CMOE_ERR_INVALID_ARG, "eps"),
     (dict(rows=(1 << 21) + 1), B.CMOE_ERR_UNSUPPORTED, "rows"),
+    (dict(d=(1 << 24) + 32), B.CMOE_ERR_UNSUPPORTED, "d >"),
+    (dict(d=2**31 - 1, h8=None, h8_scale=None), B.CMOE_ERR_UNSUPPORTED, "d >"),
     (dict(residual=None), B.CMOE_ERR_INVALID_ARG, "residual"),
     (dict(h=None, h8=None, h8_scale=None, residual_out=None), B.CMOE_ERR_INVALID_ARG, "output"),
     (dict(h8_scale=None), B.CMOE_ERR_INVALID_ARG, "together"),
