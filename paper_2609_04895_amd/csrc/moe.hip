@@ -6,14 +6,31 @@
 //   g = softmax of z over S,  y = sum_k g_k W_down,k (silu(W_gate,k x) * (W_up,k x)).
 //
 // Five launches: logits, the selection with the plan of the experts' work, W_gate
-// and W_up, W_down, the gated sum.
+// and W_up, W_down, the gated sum.  Or three, for one token and for a few that
+// hardly share an expert (each_alone): logits, W_gate and W_up with the selection
+// in front, W_down with the gated sum behind.  A small launch in between takes 4.5
+// us, whatever it does; joins within a launch (the last workgroup to arrive goes
+// on) took more, 8 to 36 us: an atomic on one address takes 7 to 11 ns, a fence
+// for other workgroups 4 to 8 us.
 //
-// The experts' weights are nearly all there is to read: 2 to 64 tokens use each
+// The experts' weights are nearly all there is to read: 1 to 64 tokens use each
 // of them for a handful of products.  So everything is made for their stream.
-// Weight rows go from HBM into LDS without passing registers, eight whole
-// 128-byte lines per instruction, and from there to the matrix core; straight
-// into its operand registers an instruction would touch sixteen lines, 16 bytes
-// at a time, and the same stream runs at 5.0 instead of 6.8 TB/s (800 MB).
+// Weight rows come from HBM eight whole 128-byte lines per instruction and pass
+// through LDS into the order in which the matrix core takes them; loaded straight
+// into its operand registers, sixteen lines per instruction and 16 bytes of each,
+// the same stream runs at 5.0 instead of 6.8 TB/s (800 MB; a plain read of it runs
+// at 7.1).  The registers hold the lines in flight, not LDS (loads that go there
+// directly): 13.1 against 11.3 us for the gate and up products of one token's eight
+// experts, 302 against 268 us for those of 64 tokens in 8 bits.
+//
+// Medians, us, of one call (N x d x F, top-K, tokens; TB/s of the weights):
+//                                  logits plan    up          down      sum
+//   128 x 2048 x 768, 8, bf16,  1    2.8         12.2 (4.1)   8.2 (3.1)
+//   128 x 2048 x 768, 8, bf16, 61    7.1   5.4  110   (6.7)  63.5 (5.8)  4.8
+//   128 x 2048 x 768, 8, 8 bit, 5    4.5   5.4   20.4 (5.6)  14.5 (3.9)  4.5
+//    32 x 2880 x 2880, 4, bf16, 16   4.6   5.4  142   (6.6)  73.5 (6.4)  4.6
+//   128 x 4096 x 1536, 8, 8 bit, 64  7.1   5.4  274   (6.0) 162   (5.1)  4.6
+// (rates: of the weights of the experts that the tokens reach.)
 #include <algorithm>
 
 #include "cmoe_internal.h"
@@ -146,6 +163,8 @@ __device__ inline int select_experts(const MoeArgs& a, int t, int lane, int coun
 // tokens of an expert.  One workgroup: what its wavefronts hand each other stays in
 // LDS.  Logits of rows behind the last token are there too; they are not waited
 // for a count that says so, only dropped.
+// Bound by latency: 5.4 us, most of it a launch's; 9 to 15 us for 64 tokens, where a
+// wavefront selects for four one after the other.
 constexpr int kPlanThreads = 1024;
 __global__ __launch_bounds__(kPlanThreads) void moe_plan_kernel(MoeArgs a) {
     __shared__ unsigned long long mask[kMaxN];    // tokens of each expert, one bit each
@@ -222,7 +241,9 @@ __global__ __launch_bounds__(kPlanThreads) void moe_plan_kernel(MoeArgs a) {
 // Logits, summed in fp64 and rounded to fp32 once after the bias, as the cache
 // step's router does: they decide the selection.  A bias of -inf takes its expert
 // out whatever the sum is.  Widening a value to fp64 takes as long as four
-// products: EG experts share each of a token's.
+// products: EG experts share each of a token's.  Bound by latency up to 16 tokens
+// (2.8 us for one, 4.5 for 16), by fp64 above (64 tokens, 128 x 4096: 7.2 us with
+// four experts by eight tokens, 13.9 with one by eight).
 // grid: x = groups of EG experts, y = groups of TG tokens; the wavefronts share the sum.
 template <bool BF16, int EG, int TG>
 __global__ __launch_bounds__(kThreads) void moe_logits_kernel(MoeArgs a) {
@@ -263,7 +284,7 @@ __global__ __launch_bounds__(kThreads) void moe_logits_kernel(MoeArgs a) {
             a.z[(int64_t)(t0 + t) * a.N + e] = b == -INFINITY ? -INFINITY : (float)(s + (double)b);
         }
     }
-    if (a.h8)  // the experts' 8-bit input as bf16, in which every value is exact; 16 values per thread
+    if (a.h8)  // the experts' 8-bit input as bf16, exact from 2^-126 on; 16 values per thread
         for (int64_t t = t0 + blockIdx.x; t < t0 + rows; t += gridDim.x)
             for (int i = threadIdx.x; i < a.d / 16; i += kThreads) {
                 const uint32_t byte = a.h8_scale[t * a.h8_scale_stride + i / 2];
@@ -300,7 +321,9 @@ __global__ __launch_bounds__(kThreads) void moe_logits_kernel(MoeArgs a) {
 // as its weights); both operands take the same order of the sum.
 //
 // The registers hold the lines in flight, CH per wavefront: line l + CH is asked
-// for when line l has gone to LDS, which holds one line at a time.
+// for when line l has gone to LDS, which holds one line at a time.  8 KB of weights
+// per wavefront and 8 to 16 wavefronts per CU: with twice as much in flight the
+// rate falls (6.8 to 6.2 TB/s), with four tiles of rows it stays.
 template <int FORMAT>
 struct Format;
 
@@ -323,7 +346,8 @@ struct Format<kMoeMx8> {
     static constexpr int kLine = 128, kParts = 2, kPlanes = 3, kBytes = 2;
     static constexpr int kReads = 2;
     __device__ static int unit(int, int j, int q) { return 2 * q + j; }  // half i is part i
-    // The weights become bf16, in which every value is exact; scales: the line's four.
+    // The weights become bf16, in which every value of 2^-126 and more in magnitude
+    // is exact; scales: the line's four.
     __device__ static f32x4 mul(const u32x4& w, uint32_t scales, int i, const u32x4* b, f32x4 c) {
         const int q = (threadIdx.x & 63) >> 4;
         const float s = __uint_as_float((scales >> (16 * i + 8 * (q >> 1)) & 255u) << 23);
@@ -518,7 +542,9 @@ struct Product {
 __device__ inline float silu_mul(float g, float u) { return g / (1.0f + expf(-g)) * u; }
 
 // fp32 as the sum of three bf16 numbers, exactly but for its last bit or two:
-// the intermediate loses nothing on the bf16 matrix core.
+// the intermediate loses nothing on the bf16 matrix core.  Rounded to bf16, the
+// tiles would take a third of the columns; its error, 2^-9 of each product, would be
+// the largest of the whole layer.
 __device__ inline void split3(float v, __bf16* p) {
     p[0] = (__bf16)v;
     const float r = fabsf((float)p[0]) < INFINITY ? v - (float)p[0] : 0.0f;
@@ -548,6 +574,9 @@ __device__ __forceinline__ void up_product(const MoeArgs& a, const uint8_t* toke
 // own: each wavefront finds its expert from the token's logits, which takes less
 // than the plan's launch, and one per token leaves the units for the down
 // projection.
+// Bound by HBM from some 200 MB on, by the start and the end of the stream below.
+// Split over the sum, so that one token's experts too (eight of 96 tiles at F = 768)
+// give every CU three workgroups.
 // grid: x = F / (8 RT), y = units
 template <int FORMAT, int RT, bool EACH>
 __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeArgs a) {
@@ -618,7 +647,9 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeArgs a) {
     }
 }
 
-// y: the gated sum over a token's experts in descending logit.
+// y: the gated sum over a token's experts in descending logit.  A launch's 4.5 us:
+// what it reads was just written.  The order of the sum is fixed, which atomics in the
+// down projection would not give.
 // grid: x = d / (4 kThreads) rounded up, y = tokens
 __global__ __launch_bounds__(kThreads) void moe_sum_kernel(MoeArgs a) {
     const int t = blockIdx.y, j = (blockIdx.x * kThreads + threadIdx.x) * 4;
@@ -736,7 +767,12 @@ __global__ __launch_bounds__(One<FORMAT>::kThreads) void moe_down_one_kernel(Moe
 }
 
 // Down projection: the workgroup's wavefronts take RT tiles of 16 rows and a part
-// of the sum each, `split` parts.
+// of the sum each, `split` parts (1, 2 and 4 parts take 63 to 65 us at 61 tokens of
+// 128 x 2048 x 768; at 61 tokens the rule takes 1).  Bound by HBM and by the
+// columns, three for each token: read through the caches, into LDS and out again.
+// Without their loads (61 tokens bf16, 64 tokens 8 bits) it takes 58 and 135
+// instead of 63 and 161 us.  Six and more tokens of an expert with 8-bit weights
+// hold one half of a line's columns at a time; both at once spill: 221 us.
 // grid: x = d / 16 / (RT kWaves / split) rounded up, y = units
 template <int FORMAT, int RT>
 __global__ __launch_bounds__(kThreads, 3) void moe_down_kernel(MoeArgs a, int split) {
