@@ -324,11 +324,22 @@ __global__ __launch_bounds__(kThreads) void moe_logits_kernel(MoeArgs a) {
 // for when line l has gone to LDS, which holds one line at a time.  8 KB of weights
 // per wavefront and 8 to 16 wavefronts per CU: with twice as much in flight the
 // rate falls (6.8 to 6.2 TB/s), with four tiles of rows it stays.
+//
+// 8-bit rows of an odd number of half lines (kMoeMx8Odd) begin in the middle of a
+// line of memory every other time: what is loaded as one line is half of two, and
+// the sum ends in half a line.  There the weights go through the caches, which keep
+// a line for its second half; elsewhere they are read once, nontemporally.  Cached
+// against nontemporal, gate and up and down: 64 tokens of 32 experts of 2880 x 2880
+// 123 and 88 against 136 and 101 us; whole lines, 64 tokens of 128 experts of 4096 x
+// 1536, 293 and 173 against 273 and 162.
+constexpr int kMoeMx8Odd = 3;
+
 template <int FORMAT>
 struct Format;
 
 template <>
 struct Format<kMoeBf16> {
+    static constexpr bool kScaled = false, kOdd = false;
     static constexpr int kLine = 64;   // values of a line of weights
     static constexpr int kParts = 1;   // 128-byte lines that these values take in a column
     static constexpr int kPlanes = 3;  // bf16 numbers of an fp32 intermediate value
@@ -343,6 +354,7 @@ struct Format<kMoeBf16> {
 
 template <>
 struct Format<kMoeMx8> {
+    static constexpr bool kScaled = true, kOdd = false;
     static constexpr int kLine = 128, kParts = 2, kPlanes = 3, kBytes = 2;
     static constexpr int kReads = 2;
     __device__ static int unit(int, int j, int q) { return 2 * q + j; }  // half i is part i
@@ -370,7 +382,13 @@ struct Format<kMoeMx8> {
 };
 
 template <>
+struct Format<kMoeMx8Odd> : Format<kMoeMx8> {
+    static constexpr bool kOdd = true;
+};
+
+template <>
 struct Format<kMoeF32> {
+    static constexpr bool kScaled = false, kOdd = false;
     static constexpr int kLine = 32, kParts = 1, kPlanes = 1, kBytes = 4, kReads = 1;
     __device__ static int unit(int i, int, int q) { return q + 4 * i; }
     __device__ static f32x4 mul(const u32x4& w, uint32_t, int, const u32x4* b, f32x4 c) {
@@ -417,18 +435,24 @@ struct Product {
     int columns, l0, l1, lines;
     char* lds;
     int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, i8 = lane >> 3, p8 = lane & 7;
-    // 8-bit rows may end in half a line: units 4 .. 7 of it would be the next row's
-    bool ragged = FORMAT == kMoeMx8 && tiles.pitch % 128 != 0;
 
-    __device__ __forceinline__ bool half(int l) const { return ragged && l == lines - 1; }
+    // the last line of a row is half a line: units 4 .. 7 of it would be the next row's
+    __device__ __forceinline__ bool half(int l) const { return P::kOdd && l == lines - 1; }
+
+    __device__ __forceinline__ static u32x4 load_unit(const char* p) {
+        const u32x4* u = reinterpret_cast<const u32x4*>(p);
+        if constexpr (P::kOdd)
+            return *u;
+        else
+            return __builtin_nontemporal_load(u);
+    }
 
     __device__ __forceinline__ void load_weights(Line& v, int l) const {
         const int64_t at = i8 * tiles.pitch + (int64_t)l * 128 + (half(l) ? p8 & 3 : p8) * 16;
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
-            // weights are read once: nontemporal
-            v.w[t][0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tiles.w0 + t * tiles.next + at));
-            if (!HALF) v.w[t][HALF ? 0 : 1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(tiles.w1 + t * tiles.next + at));
+            v.w[t][0] = load_unit(tiles.w0 + t * tiles.next + at);
+            if (!HALF) v.w[t][HALF ? 0 : 1] = load_unit(tiles.w1 + t * tiles.next + at);
         }
     }
     // part k of the columns
@@ -441,11 +465,11 @@ struct Product {
     // lane 4 i + p loads the four scales of row i and pair p, a (tile, line) of a
     // batch of CH lines from l: the lanes of a row's neighbouring lines share a lookup
     __device__ __forceinline__ uint32_t load_scales(int l) const {
-        if constexpr (FORMAT != kMoeMx8) return 0;
-        static_assert(FORMAT != kMoeMx8 || (CH * RT <= 4 && !HALF), "four pairs of whole tiles at most");
+        if constexpr (!P::kScaled) return 0;
+        static_assert(!P::kScaled || (CH * RT <= 4 && !HALF), "four pairs of whole tiles at most");
         const int t = min((lane & 3) / CH, RT - 1), at = min(l + (lane & 3) % CH, l1 - 1);
         const uint8_t* p = (lane < 32 ? tiles.s0 : tiles.s1) + ((lane >> 2) & 7) * (tiles.pitch / 32) + t * (tiles.next / 32) + 4 * at;
-        if (!ragged) return *reinterpret_cast<const uint32_t*>(p);
+        if constexpr (!P::kOdd) return *reinterpret_cast<const uint32_t*>(p);
         const uint16_t *lo = reinterpret_cast<const uint16_t*>(p), *hi = lo + (at == lines - 1 ? 0 : 1);
         return *lo | (uint32_t)*hi << 16;
     }
@@ -462,7 +486,7 @@ struct Product {
             if (!HALF) *reinterpret_cast<u32x4*>(to + t * 2048 + 1024) = v.w[t][HALF ? 0 : 1];
         }
         uint32_t four[RT] = {};
-        if constexpr (FORMAT == kMoeMx8)
+        if constexpr (P::kScaled)
 #pragma unroll
             for (int t = 0; t < RT; ++t) four[t] = (uint32_t)__shfl((int)scales, 4 * r + t * CH + i);
         // halves of the line: both at once, or one after the other
@@ -610,8 +634,8 @@ __global__ __launch_bounds__(kThreads, 4) void moe_up_kernel(MoeArgs a) {
     Tiles tiles;
     tiles.w0 = static_cast<const char*>(a.experts) + row * pitch;
     tiles.w1 = tiles.w0 + a.F * pitch;
-    tiles.s0 = FORMAT == kMoeMx8 ? a.scales + row * (pitch / 32) : nullptr;
-    tiles.s1 = FORMAT == kMoeMx8 ? tiles.s0 + a.F * (pitch / 32) : nullptr;
+    tiles.s0 = P::kScaled ? a.scales + row * (pitch / 32) : nullptr;
+    tiles.s1 = P::kScaled ? tiles.s0 + a.F * (pitch / 32) : nullptr;
     tiles.pitch = pitch;
     tiles.next = 8 * pitch;
     const int lines = (a.d + P::kLine - 1) / P::kLine, l0 = wv * lines / kWaves, l1 = (wv + 1) * lines / kWaves;
@@ -705,8 +729,8 @@ __device__ __forceinline__ Tiles down_tiles(const MoeArgs& a, int expert, int ro
     Tiles t;
     t.w0 = static_cast<const char*>(a.experts) + before;
     t.w1 = t.w0 + 8 * pitch;
-    t.s0 = FORMAT == kMoeMx8 ? a.scales + before / 32 : nullptr;
-    t.s1 = FORMAT == kMoeMx8 ? t.s0 + 8 * (pitch / 32) : nullptr;
+    t.s0 = P::kScaled ? a.scales + before / 32 : nullptr;
+    t.s1 = P::kScaled ? t.s0 + 8 * (pitch / 32) : nullptr;
     t.pitch = pitch;
     t.next = 16 * pitch;
     return t;
@@ -717,11 +741,11 @@ __device__ __forceinline__ Tiles down_tiles(const MoeArgs& a, int expert, int ro
 // give all CUs a workgroup at d = 2048, for weights of 16 and 32 bits (2048 x 768
 // bf16, eight experts: 8.5 us against 9.8 with whole ones), whole tiles for 8-bit
 // weights, of which half tiles put too few bytes in flight (2880 x 2880, four
-// experts: 14.3 us against 16.6).
+// experts, nontemporal: 14.3 us against 16.6).
 // grid: x = d / kTile, y = tokens
 template <int FORMAT>
 struct One {
-    static constexpr bool kHalf = FORMAT != kMoeMx8;
+    static constexpr bool kHalf = !Format<FORMAT>::kScaled;
     static constexpr int kTile = kHalf ? 8 : 16, kThreads = kHalf ? 512 : 1024, kWaves = kThreads / 64;
 };
 
@@ -842,34 +866,48 @@ bool each_alone(const MoeArgs& a) {
     return a.T == 1 || (a.T <= 4 && 4 * rows <= a.N && bytes <= (a.format == kMoeMx8 ? 96 : 256) * 1000000ll);
 }
 
+// The two products, with their variants for rows of whole lines or not.
+template <int FORMAT, int RT, bool EACH>
+void launch_up(const MoeArgs& a, int units, hipStream_t st) {
+    launch_kernel(moe_up_kernel<FORMAT, RT, EACH>, dim3(a.F / (8 * RT), units), dim3(kThreads), st, Timing{}, a);
+}
+
 template <int FORMAT>
+void launch_down_one(const MoeArgs& a, hipStream_t st) {
+    using O = One<FORMAT>;
+    const int lines = (a.F + Format<FORMAT>::kLine - 1) / Format<FORMAT>::kLine;
+    int split = 1;
+    while (2 * split * a.K <= O::kWaves && 2 * split <= lines) split *= 2;
+    launch_kernel(moe_down_one_kernel<FORMAT>, dim3(a.d / O::kTile, a.T), dim3(O::kThreads), st, Timing{}, a, split);
+}
+
+template <int FORMAT, int RT>
+void launch_down(const MoeArgs& a, int units, hipStream_t st) {
+    const int lines = (a.F + Format<FORMAT>::kLine - 1) / Format<FORMAT>::kLine;
+    // parts of the sum: four lines at least, more parts where the tiles alone do not
+    // fill the device
+    int split = lines >= 32 ? 4 : lines >= 16 ? 2 : 1;
+    while (split < kWaves && (int64_t)(a.d / 16) * units * split < 4096) split *= 2;
+    const int tiles = RT * kWaves / split;
+    launch_kernel(moe_down_kernel<FORMAT, RT>, dim3((a.d / 16 + tiles - 1) / tiles, units), dim3(kThreads), st, Timing{}, a, split);
+}
+
+// UP, DOWN: the formats of W_gate's and W_up's rows and of W_down's.
+template <int UP, int DOWN>
 void launch_experts(const MoeArgs& a, hipStream_t st) {
     const int rows = a.T * a.K, units = moe_max_units(rows, a.N);
-    const int lines = (a.F + Format<FORMAT>::kLine - 1) / Format<FORMAT>::kLine;
     if (each_alone(a)) {
-        launch_kernel(moe_up_kernel<FORMAT, 1, true>, dim3(a.F / 8, rows), dim3(kThreads), st, Timing{}, a);
-        int split = 1;
-        while (2 * split * a.K <= One<FORMAT>::kWaves && 2 * split <= lines) split *= 2;
-        launch_kernel(moe_down_one_kernel<FORMAT>, dim3(a.d / One<FORMAT>::kTile, a.T), dim3(One<FORMAT>::kThreads), st, Timing{}, a,
-                      split);
+        launch_up<UP, 1, true>(a, rows, st);
+        launch_down_one<DOWN>(a, st);
         return;
     }
     launch_kernel(moe_plan_kernel, dim3(1), dim3(kPlanThreads), st, Timing{}, a);
-    const bool few = (int64_t)(a.F / 16) * units < 1024;
-    if (few)
-        launch_kernel(moe_up_kernel<FORMAT, 1, false>, dim3(a.F / 8, units), dim3(kThreads), st, Timing{}, a);
-    else
-        launch_kernel(moe_up_kernel<FORMAT, 2, false>, dim3(a.F / 16, units), dim3(kThreads), st, Timing{}, a);
-    // parts of the down sum: four lines at least, more parts where the tiles alone
-    // do not fill the device
-    int split = lines >= 32 ? 4 : lines >= 16 ? 2 : 1;
-    while (split < kWaves && (int64_t)(a.d / 16) * units * split < 4096) split *= 2;
-    if (few) {
-        const int tiles = kWaves / split;
-        launch_kernel(moe_down_kernel<FORMAT, 1>, dim3((a.d / 16 + tiles - 1) / tiles, units), dim3(kThreads), st, Timing{}, a, split);
+    if ((int64_t)(a.F / 16) * units < 1024) {  // few tiles: one for each wavefront
+        launch_up<UP, 1, false>(a, units, st);
+        launch_down<DOWN, 1>(a, units, st);
     } else {
-        const int tiles = 2 * kWaves / split;
-        launch_kernel(moe_down_kernel<FORMAT, 2>, dim3((a.d / 16 + tiles - 1) / tiles, units), dim3(kThreads), st, Timing{}, a, split);
+        launch_up<UP, 2, false>(a, units, st);
+        launch_down<DOWN, 2>(a, units, st);
     }
     launch_kernel(moe_sum_kernel, dim3((a.d / 4 + kThreads - 1) / kThreads, a.T), dim3(kThreads), st, Timing{}, a);
 }
@@ -882,11 +920,13 @@ hipError_t launch_moe(const MoeArgs& a, hipStream_t st) {
     else
         launch_route<false>(a, st);
     if (a.format == kMoeF32)
-        launch_experts<kMoeF32>(a, st);
+        launch_experts<kMoeF32, kMoeF32>(a, st);
     else if (a.format == kMoeBf16)
-        launch_experts<kMoeBf16>(a, st);
+        launch_experts<kMoeBf16, kMoeBf16>(a, st);
+    else if (a.d % 128 == 0)
+        a.F % 128 == 0 ? launch_experts<kMoeMx8, kMoeMx8>(a, st) : launch_experts<kMoeMx8, kMoeMx8Odd>(a, st);
     else
-        launch_experts<kMoeMx8>(a, st);
+        a.F % 128 == 0 ? launch_experts<kMoeMx8Odd, kMoeMx8>(a, st) : launch_experts<kMoeMx8Odd, kMoeMx8Odd>(a, st);
     return hipGetLastError();
 }
 
