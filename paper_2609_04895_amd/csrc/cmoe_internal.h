@@ -249,6 +249,7 @@ struct MoeArgs {
     MoePlan* plan;
     float* z;               // [T][N]   logits
     float* gate;            // [T][K]   -1: no expert is selected here
+    int32_t* expert;        // [T][K]   selected experts, where a launch of their own selects
     uint16_t* x;            // [T][d]   bf16 values of h8
     void* act;              // SwiGLU intermediate of each (expert, token), in that order: [3][F] bf16 or [F] fp32
     float* out;             // [T][K][d] expert outputs

@@ -117,7 +117,7 @@ bool norm_aligned(const cmoe::NormArgs& a) {
 
 // Offsets of the workspace's parts.
 struct Parts {
-    size_t plan, z, gate, h, h8, h8_scale, x, act, out, total;
+    size_t plan, z, gate, expert, h, h8, h8_scale, x, act, out, total;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -156,6 +156,7 @@ Parts moe_parts(const cmoe_moe_config* c) {
     p.plan = take(sizeof(cmoe::MoePlan));
     p.z = take(T * c->N * 4);
     p.gate = take(rows * 4);
+    p.expert = take(rows * 4);
     p.h = take(T * d * e);
     p.h8 = take(a8 ? T * d : 0);
     p.h8_scale = take(a8 ? T * d / 32 : 0);
@@ -222,6 +223,7 @@ cmoe_status run_layer(cmoe_moe* m, const cmoe_moe_call* c, const void* h, int64_
     a.plan = reinterpret_cast<cmoe::MoePlan*>(m->ws + m->parts.plan);
     a.z = reinterpret_cast<float*>(m->ws + m->parts.z);
     a.gate = reinterpret_cast<float*>(m->ws + m->parts.gate);
+    a.expert = reinterpret_cast<int32_t*>(m->ws + m->parts.expert);
     a.x = reinterpret_cast<uint16_t*>(m->ws + m->parts.x);
     a.act = m->ws + m->parts.act;
     a.out = reinterpret_cast<float*>(m->ws + m->parts.out);

@@ -5,8 +5,8 @@
 //   z = W_r h + b,  S = the K largest z (lower index on equal ones),
 //   g = softmax of z over S,  y = sum_k g_k W_down,k (silu(W_gate,k x) * (W_up,k x)).
 //
-// Five launches: logits, the selection with the plan of the experts' work, W_gate
-// and W_up, W_down, the gated sum.  Or three, for one token and for a few that
+// Five launches: logits, the selection with the plan of the experts' work (above 32
+// tokens a launch each), W_gate and W_up, W_down, the gated sum.  Or three, for one token and for a few that
 // hardly share an expert (each_alone): logits, W_gate and W_up with the selection
 // in front, W_down with the gated sum behind.  A small launch in between takes 4.5
 // us, whatever it does; joins within a launch (the last workgroup to arrive goes
@@ -26,10 +26,10 @@
 // Medians, us, of one call (N x d x F, top-K, tokens; TB/s of the weights):
 //                                  logits plan    up          down      sum
 //   128 x 2048 x 768, 8, bf16,  1    2.8         12.2 (4.1)   8.2 (3.1)
-//   128 x 2048 x 768, 8, bf16, 61    7.1   5.4  110   (6.7)  63.5 (5.8)  4.8
+//   128 x 2048 x 768, 8, bf16, 61    7.1   9.5  110   (6.7)  63.5 (5.8)  4.8
 //   128 x 2048 x 768, 8, 8 bit, 5    4.5   5.4   20.4 (5.6)  14.5 (3.9)  4.5
 //    32 x 2880 x 2880, 4, bf16, 16   4.6   5.4  142   (6.6)  73.5 (6.4)  4.6
-//   128 x 4096 x 1536, 8, 8 bit, 64  7.1   5.4  274   (6.0) 162   (5.1)  4.6
+//   128 x 4096 x 1536, 8, 8 bit, 64  7.1   9.5  274   (6.0) 162   (5.1)  4.6
 // (rates: of the weights of the experts that the tokens reach.)
 #include <algorithm>
 
@@ -159,13 +159,26 @@ __device__ inline int select_experts(const MoeArgs& a, int t, int lane, int coun
     return e;
 }
 
+// The selection on its own, a token per workgroup.  For more than two tokens per
+// wavefront of the plan's one workgroup this is the faster way in spite of its
+// launch: top-8 of 128, 64 tokens 4.7 and 4.8 us against 15, 32 tokens 9.5 both ways.
+__global__ __launch_bounds__(64) void moe_select_kernel(MoeArgs a) {
+    const int t = blockIdx.x, lane = threadIdx.x;
+    if (t >= live_tokens(a)) return;
+    const int e = select_experts(a, t, lane, a.K, true);
+    if (lane < a.K) a.expert[t * a.K + lane] = e;
+}
+
 // Selection of all tokens and the plan of the experts' work, units of up to 16
 // tokens of an expert.  One workgroup: what its wavefronts hand each other stays in
 // LDS.  Logits of rows behind the last token are there too; they are not waited
 // for a count that says so, only dropped.
-// Bound by latency: 5.4 us, most of it a launch's; 9 to 15 us for 64 tokens, where a
-// wavefront selects for four one after the other.
+// Bound by latency: 5.4 us, most of it a launch's, and by the instructions of the
+// selections on one CU above 16 tokens.
+//
+// SELECTED: moe_select_kernel has selected.
 constexpr int kPlanThreads = 1024;
+template <bool SELECTED>
 __global__ __launch_bounds__(kPlanThreads) void moe_plan_kernel(MoeArgs a) {
     __shared__ unsigned long long mask[kMaxN];    // tokens of each expert, one bit each
     __shared__ uint8_t place[kMaxN][kMoeTokens];  // of the expert in the token's selection
@@ -175,11 +188,17 @@ __global__ __launch_bounds__(kPlanThreads) void moe_plan_kernel(MoeArgs a) {
     const int n = live_tokens(a);
     if (tid < kMaxN) mask[tid] = 0;
     __syncthreads();
-    for (int t = tid >> 6; t < a.T; t += kPlanThreads / 64) {
-        const int e = select_experts(a, t, lane, a.K, t < n);
-        if (lane < a.K && e >= 0 && t < n) {
-            place[e][t] = (uint8_t)lane;
-            atomicOr(&mask[e], 1ull << t);
+    auto add = [&](int t, int k, int e) {
+        if (e < 0) return;
+        place[e][t] = (uint8_t)k;
+        atomicOr(&mask[e], 1ull << t);
+    };
+    if constexpr (SELECTED) {
+        for (int i = tid; i < n * a.K; i += kPlanThreads) add(i / a.K, i % a.K, a.expert[i]);
+    } else {
+        for (int t = tid >> 6; t < a.T; t += kPlanThreads / 64) {
+            const int e = select_experts(a, t, lane, a.K, t < n);
+            if (lane < a.K && t < n) add(t, lane, e);
         }
     }
     __syncthreads();
@@ -901,7 +920,12 @@ void launch_experts(const MoeArgs& a, hipStream_t st) {
         launch_down_one<DOWN>(a, st);
         return;
     }
-    launch_kernel(moe_plan_kernel, dim3(1), dim3(kPlanThreads), st, Timing{}, a);
+    if (a.T > 2 * kPlanThreads / 64) {
+        launch_kernel(moe_select_kernel, dim3(a.T), dim3(64), st, Timing{}, a);
+        launch_kernel(moe_plan_kernel<true>, dim3(1), dim3(kPlanThreads), st, Timing{}, a);
+    } else {
+        launch_kernel(moe_plan_kernel<false>, dim3(1), dim3(kPlanThreads), st, Timing{}, a);
+    }
     if ((int64_t)(a.F / 16) * units < 1024) {  // few tiles: one for each wavefront
         launch_up<UP, 1, false>(a, units, st);
         launch_down<DOWN, 1>(a, units, st);
