@@ -456,8 +456,12 @@ def quantize_experts(experts):
     L, N, n = experts.shape
     q = torch.empty((L, N, n), dtype=torch.uint8, device=experts.device)
     scale = torch.empty((L, N, n // 32), dtype=torch.uint8, device=experts.device)
-    for l in range(L):  # a call takes 2^34 values, a whole model's pool has more
-        cmoe_quantize(experts[l], q[l], scale[l])
+    # one long row of whole blocks, in calls of 2^34 values, the most that one takes
+    total, step = experts.numel(), 1 << 34
+    src, qs, ss = experts.view(1, total), q.view(1, total), scale.view(1, total // 32)
+    for at in range(0, total, step):
+        end = min(at + step, total)
+        cmoe_quantize(src[:, at:end], qs[:, at:end], ss[:, at // 32:end // 32])
     return q, scale
 
 
