@@ -361,6 +361,13 @@ def _invalid(msg):
     raise CmoeError(CMOE_ERR_INVALID_ARG, msg)
 
 
+def _pack(fields, *values):
+    try:
+        return fields.pack(*values)
+    except struct.error as e:  # a number that is not a whole one or that its field cannot hold
+        _invalid(f"an argument is out of range: {e}")
+
+
 def _rows(t, name, dtype, shape, dev):
     """Address and row stride of a tensor [rows][cols] of device `dev` whose rows
     are contiguous; raises on any other tensor."""
@@ -417,7 +424,7 @@ def _norm_args(residual, delta, weight, eps, residual_out, h, h8, h8_scale, n_ro
         pc, pcs = _rows(h8_scale, "h8_scale", torch.uint8, (rows, d // 32), dev)
     if n_rows is not None:
         pn = _flat(n_rows, "n_rows", torch.int32, 1, dev)
-    return _NORM.pack(rows, d, types[dt], delta_dtype, eps, p, ps, pd, pds, po, pos, pw, ph, phs, p8, p8s, pc, pcs, pn)
+    return _pack(_NORM, rows, d, types[dt], delta_dtype, eps, p, ps, pd, pds, po, pos, pw, ph, phs, p8, p8s, pc, pcs, pn)
 
 
 def cmoe_add_norm(residual, delta=None, weight=None, eps=1e-6, residual_out=None, h=None, h8=None, h8_scale=None,
@@ -531,7 +538,7 @@ class MoeLayers:
             psel = _flat(selected, "selected", torch.int32, rows * self.K, dev)
         if gates is not None:
             pg = _flat(gates, "gates", torch.float32, rows * self.K, dev)
-        return _CALL.pack(layer, rows, ph, phs, p8, p8s, pc, pcs, py, pys, pn, psel, pg)
+        return _pack(_CALL, layer, rows, ph, phs, p8, p8s, pc, pcs, py, pys, pn, psel, pg)
 
     def cmoe_moe_layer(self, layer, h, y, h8=None, h8_scale=None, n_tokens=None, selected=None, gates=None):
         """y [T][d] = the layer's output for the hidden states h [T][d]; the

@@ -37,3 +37,36 @@ def test_quantize_experts_covers_pools_of_any_size(monkeypatch, L, N, n):
         assert start == at
         at += count
     assert at == L * N * n
+
+
+def layers_on_the_host():
+    """A MoeLayers without a library handle, on host tensors: its calls pack their
+    arguments and are refused by the library at the latest."""
+    m = object.__new__(B.MoeLayers)
+    m.handle, m.device, m.L, m.K, m.d, m.dtype = None, -1, 2, 2, 64, torch.bfloat16
+    m.norm_weight, m.norm_eps = None, 1e-6
+    return m
+
+
+@pytest.mark.parametrize("eps", [1e39, -1e300, float("inf"), float("nan")])
+def test_norm_eps_that_fp32_cannot_hold(eps):
+    r = torch.zeros((4, 64))
+    with pytest.raises(B.CmoeError) as err:
+        B.cmoe_add_norm(r, eps=eps, residual_out=r)
+    assert err.value.status == B.CMOE_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("layer", [1 << 31, -(1 << 31) - 1, 1 << 80, 0.5])
+def test_layers_that_no_argument_can_hold(layer):
+    m, h, y = layers_on_the_host(), torch.zeros((4, 64), dtype=torch.bfloat16), torch.zeros((4, 64))
+    for call in (lambda: m.cmoe_moe_layer(layer, h, y), lambda: m.cmoe_moe_block(layer, h, None, y)):
+        with pytest.raises(B.CmoeError) as err:
+            call()
+        assert err.value.status == B.CMOE_ERR_INVALID_ARG
+
+
+def test_rows_that_no_argument_can_hold():
+    r = torch.empty((1 << 31, 1), device="meta").as_strided((1 << 31, 1), (1, 1))
+    with pytest.raises(B.CmoeError) as err:
+        B.cmoe_add_norm(r, residual_out=r)
+    assert err.value.status == B.CMOE_ERR_INVALID_ARG
