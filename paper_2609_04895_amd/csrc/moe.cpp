@@ -3,9 +3,11 @@
 // for a few tokens; validation, the workspace and the launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 #include <new>
 
 #include "../../include/cmoe.h"
@@ -28,6 +30,13 @@ cmoe_status hip_fail(hipError_t e, const char* where) {
 }
 
 bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// Whether no output has the place of an input or of another output (NULL: not given).
+bool own_places(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+    for (auto o = outputs.begin(); o != outputs.end(); ++o)
+        if (*o && (std::find(inputs.begin(), inputs.end(), *o) != inputs.end() || std::find(outputs.begin(), o, *o) != o)) return false;
+    return true;
+}
 
 // A launch goes to the current device, so the stream has to be one of its own.
 cmoe_status check_stream(hipStream_t st, int device) {
@@ -83,10 +92,8 @@ cmoe_status check_norm(const cmoe_norm* n, bool outputs) {
     // every element is read and written by one thread: in place is fine for the sum only
     if (n->residual_out == n->residual && n->residual && n->residual_out_stride != n->residual_stride)
         return fail(CMOE_ERR_INVALID_ARG, "norm: in place, the two residual strides must be equal");
-    for (const void* out : {static_cast<const void*>(n->h), static_cast<const void*>(n->h8), static_cast<const void*>(n->h8_scale)})
-        for (const void* other : {n->residual, n->delta, static_cast<const void*>(n->residual_out), n->weight})
-            if (out && out == other) return fail(CMOE_ERR_INVALID_ARG, "norm: an output has the place of an input or another output");
-    if (n->residual_out && (n->residual_out == n->delta || n->residual_out == n->weight))
+    if (!own_places({n->h, n->h8, n->h8_scale, n->residual_out}, {n->delta, n->weight, n->n_rows}) ||
+        !own_places({n->h, n->h8, n->h8_scale}, {n->residual}))
         return fail(CMOE_ERR_INVALID_ARG, "norm: an output has the place of an input or another output");
     return CMOE_OK;
 }
@@ -332,7 +339,8 @@ cmoe_status cmoe_moe_layer(cmoe_moe* m, const cmoe_moe_call* c) {
         return fail(CMOE_ERR_INVALID_ARG, "a row stride of h8 or h8_scale is less than the row");
     if (a8 && (!aligned_to(c->h8, 16) || c->h8_stride % 16)) return fail(CMOE_ERR_UNSUPPORTED, "rows of h8 must be 16-byte aligned");
     if (!a8 && (c->h8 || c->h8_scale)) return fail(CMOE_ERR_INVALID_ARG, "h8 is given, but the configuration's activations are not 8-bit");
-    if (static_cast<const void*>(c->y) == c->h) return fail(CMOE_ERR_INVALID_ARG, "y has the place of h");
+    if (!own_places({c->y, c->selected, c->gates}, {c->h, c->h8, c->h8_scale, c->n_tokens}))
+        return fail(CMOE_ERR_INVALID_ARG, "an output has the place of an input or another output");
     return run_layer(m, c, c->h, c->h_stride, c->h8, c->h8_stride, c->h8_scale, c->h8_scale_stride);
 }
 
@@ -348,8 +356,10 @@ cmoe_status cmoe_moe_block(cmoe_moe* m, const cmoe_norm* n, const cmoe_moe_call*
     if (n->h || n->h8 || n->h8_scale) return fail(CMOE_ERR_INVALID_ARG, "norm: h goes through the workspace: h, h8 and h8_scale must be NULL");
     if (n->n_rows) return fail(CMOE_ERR_INVALID_ARG, "norm: the number of rows is the call's n_tokens");
     if ((st = check_norm(n, false)) != CMOE_OK) return st;
-    if (c->y && (c->y == n->residual || c->y == n->residual_out)) return fail(CMOE_ERR_INVALID_ARG, "y has the place of the residual");
     if (c->T == 0) return CMOE_OK;
+    if (!own_places({c->y, c->selected, c->gates, n->residual_out}, {n->weight, c->n_tokens}) ||
+        !own_places({c->y, c->selected, c->gates}, {n->residual}) || !own_places({c->selected, c->gates}, {n->delta}))
+        return fail(CMOE_ERR_INVALID_ARG, "an output has the place of an input or another output");
     cmoe::NormArgs a = norm_args(n);
     const bool a8 = g.activations == CMOE_FORMAT_MX8;
     a.n_rows = c->n_tokens;
