@@ -5,7 +5,7 @@
 // One pass over the data: each thread keeps its values of a row in registers
 // between the sum of squares and the outputs, so every input is read and every
 // output written once.  Both kernels are bound by HBM for many rows (8192 rows of
-// 2880 bf16 values with an fp32 delta: 48 us, 5.4 TB/s; 604 million values into 8
+// 2880 bf16 values with an fp32 delta: 47.7 us, 5.5 TB/s; 604 million values into 8
 // bits: 294 us, 6.2 TB/s) and by the launch and one trip to memory for few (one row
 // of 2048: 2.6 us).
 //
@@ -32,10 +32,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 // Eight consecutive values, widened to fp32.  NT: nontemporal, where there are so
-// many that the caches do not hold them until they are used again: the norm's
-// outputs from 1024 rows on (8192 rows of 2880: 51.9 us against 55.8; its inputs
-// too: 56.2), all of quantize from 2^26 values on (604 million bf16 values 301 us
-// against 311; 1.4 million fp32 values 4.5 us against 3.0).
+// many that the caches would not keep them: the norm's outputs from kNormNT bytes on,
+// all of quantize from 2^26 values on (604 million bf16 values 301 us against 311;
+// 1.4 million fp32 values 4.5 us against 3.0).
 template <bool NT, typename V>
 __device__ inline V get(const void* p) {
     if constexpr (NT)
@@ -160,14 +159,13 @@ constexpr int kThreads = 256;  // threads of a workgroup with one wavefront per 
 // d % 8 == 0 and every row 16-byte aligned.  TPR threads per row, thread t taking
 // the groups of 8 values t, t + TPR, ... (NV at most); the four groups of a block
 // of 32 lie in neighbouring lanes.
-template <bool BF16, int DELTA, int TPR, int NV>
+template <bool BF16, int DELTA, int TPR, int NV, bool NT>
 __global__ __launch_bounds__(TPR > kThreads ? TPR : kThreads) void norm_kernel(NormArgs a) {
     __shared__ double red[TPR > 64 ? TPR / 64 : 1];
     constexpr int RPG = TPR >= kThreads ? 1 : kThreads / TPR;  // rows per workgroup
     const int t = threadIdx.x % TPR;
     const int64_t row = (int64_t)blockIdx.x * RPG + threadIdx.x / TPR;
     if (row >= live_rows(a)) return;  // whole wavefronts, and whole workgroups where they share a row
-    constexpr bool NT = TPR == 64;  // the launch for many rows
     const int ng = a.d / 8;
     float r[NV][8] = {};
     double ss = 0.0;
@@ -268,34 +266,56 @@ __global__ __launch_bounds__(kThreads) void norm_any_kernel(NormArgs a) {
     }
 }
 
-template <bool BF16, int DELTA>
-hipError_t launch_norm_t(const NormArgs& a, bool aligned, hipStream_t st) {
+// Bytes of outputs from which they are written nontemporally: an XCD's L2.  Cached /
+// nontemporal, us, behind a kernel that writes delta and before one that reads h (bf16,
+// fp32 delta, all three outputs): 1024 x 256 (1.3 MB) 3.4 / 3.5, 2048 x 512 (5.2 MB)
+// 4.3 / 4.2, 2048 x 1024 (10 MB) 6.7 / 6.6, 2048 x 2880 (29 MB) 16.1 / 14.3, 8192 x 4096
+// (168 MB) 73.8 / 60.8; on its own 8192 x 2880 52.7 / 48.1.
+constexpr int64_t kNormNT = 1 << 22;
+
+template <bool BF16, int DELTA, bool NT>
+void launch_rows(const NormArgs& a, hipStream_t st) {
     const int ng = a.d / 8;
     auto go = [&](auto kernel, int tpr) {
         const int rpg = tpr >= kThreads ? 1 : kThreads / tpr;
         launch_kernel(kernel, dim3((unsigned)((a.rows + rpg - 1) / rpg)), dim3(tpr > kThreads ? tpr : kThreads), st, Timing{}, a);
     };
-    if (!aligned || ng > 4096)
-        go(norm_any_kernel<BF16, DELTA>, kThreads);
-    else if (a.rows >= 1024 && ng <= 512) {
-        if (ng <= 64)
-            go(norm_kernel<BF16, DELTA, 64, 1>, 64);
-        else if (ng <= 128)
-            go(norm_kernel<BF16, DELTA, 64, 2>, 64);
-        else if (ng <= 256)
-            go(norm_kernel<BF16, DELTA, 64, 4>, 64);
-        else if (ng <= 384)
-            go(norm_kernel<BF16, DELTA, 64, 6>, 64);
-        else
-            go(norm_kernel<BF16, DELTA, 64, 8>, 64);
-    } else if (ng <= 256)
-        go(norm_kernel<BF16, DELTA, 256, 1>, 256);
+    // A wavefront per row for many narrow ones, a workgroup otherwise.  Wavefront /
+    // workgroup, us, bf16 rows, in the order of kernels above:
+    //   rows of  512: 1024 rows 3.7 / 3.7, 4096 6.4 / 7.8, 16384 18.0 / 26.3
+    //           1024: 1024 5.1 / 4.4, 2048 6.6 / 6.6, 4096 9.5 / 11.4, 12000 24.6 / 27.2
+    //           2048: 1024 8.7 / 6.5, 3000 15.1 / 15.0, 4096 15.6 / 18.1, 6000 22.2 / 23.7, 8192 33.0 / 30.5
+    //           2880: 3000 18.4 / 19.7, 4096 22.5 / 25.5, 5000 27.0 / 29.8, 6000 37.3 / 34.4, 16384 95.8 / 92.6
+    //           4096: 1024 15.0 / 9.6, 4096 30.4 / 32.7, 8192 61.9 / 60.8, 16384 147 / 131
+    // (on their own, 4096 rows of 4096 31.3 / 31.2.)
+    if (ng <= 64 && a.rows >= 1024)
+        go(norm_kernel<BF16, DELTA, 64, 1, NT>, 64);
+    else if (ng <= 128 && a.rows >= 2048)
+        go(norm_kernel<BF16, DELTA, 64, 2, NT>, 64);
+    else if (ng <= 256 && a.rows >= 4096 && a.rows < 6144)
+        go(norm_kernel<BF16, DELTA, 64, 4, NT>, 64);
+    else if (ng <= 384 && a.rows >= 4096 && a.rows < 6144)
+        go(norm_kernel<BF16, DELTA, 64, 6, NT>, 64);
+    else if (ng <= 256)
+        go(norm_kernel<BF16, DELTA, 256, 1, NT>, 256);
     else if (ng <= 512)
-        go(norm_kernel<BF16, DELTA, 256, 2>, 256);
+        go(norm_kernel<BF16, DELTA, 256, 2, NT>, 256);
     else if (ng <= 1024)
-        go(norm_kernel<BF16, DELTA, 1024, 1>, 1024);
+        go(norm_kernel<BF16, DELTA, 1024, 1, NT>, 1024);
     else
-        go(norm_kernel<BF16, DELTA, 1024, 4>, 1024);
+        go(norm_kernel<BF16, DELTA, 1024, 4, NT>, 1024);
+}
+
+template <bool BF16, int DELTA>
+hipError_t launch_norm_t(const NormArgs& a, bool aligned, hipStream_t st) {
+    const int e = BF16 ? 2 : 4;
+    const int64_t bytes = (int64_t)a.rows * a.d * ((a.residual_out ? e : 0) + (a.h ? e : 0) + (a.h8 ? 1 : 0));
+    if (!aligned || a.d / 8 > 4096)
+        launch_kernel(norm_any_kernel<BF16, DELTA>, dim3((unsigned)a.rows), dim3(kThreads), st, Timing{}, a);
+    else if (bytes >= kNormNT)
+        launch_rows<BF16, DELTA, true>(a, st);
+    else
+        launch_rows<BF16, DELTA, false>(a, st);
     return hipGetLastError();
 }
 

@@ -50,3 +50,29 @@ def test_norm_over_the_whole_range_of_fp32(scale, wscale, eps, rows, d, dtype):
             want, _, byte = ref.quantize(h.cpu())
             assert torch.equal(kw["h8_scale"].cpu().int(), byte.int())
             assert torch.equal(kw["h8"].cpu().view(torch.float8_e4m3fn).double(), want)
+
+
+# every launch shape at its borders: a wavefront or a workgroup per row, cached and
+# nontemporal outputs
+@pytest.mark.parametrize("rows,d", [(1023, 512), (1024, 512), (1024, 520), (2047, 1024), (2048, 1024), (2049, 1032), (4095, 1032),
+                                    (4096, 2048), (6143, 1536), (6144, 1536), (4097, 2880), (6143, 2080), (4096, 3080), (1030, 8192),
+                                    (300, 8200)])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_norm_launch_shapes(rows, d, dtype):
+    from paper_2609_04895_amd import cmoe as B
+    say("norm shapes", rows, d, dtype)
+    g = torch.Generator(device="cuda").manual_seed(stable_seed(f"shapes {rows} {d}"))
+    res = (torch.randn((rows, d), generator=g, device="cuda") * 4).to(dtype)
+    delta, w = torch.randn((rows, d), generator=g, device="cuda"), (1 + 0.1 * torch.randn(d, generator=g, device="cuda")).to(dtype)
+    out, h = torch.empty_like(res), torch.empty_like(res)
+    kw = {}
+    if d % 32 == 0:
+        kw = dict(h8=torch.empty((rows, d), dtype=torch.uint8, device="cuda"),
+                  h8_scale=torch.empty((rows, d // 32), dtype=torch.uint8, device="cuda"))
+    B.cmoe_add_norm(res, delta, w, 2.0 ** -20, residual_out=out, h=h, **kw)
+    r, h64 = ref.norm(res.cpu(), delta.cpu(), w.cpu(), 2.0 ** -20)
+    assert torch.equal(out.cpu(), r)
+    off = (h.cpu().double() - h64).abs()
+    assert (off <= 2.0 ** -24 * (1 + 2.0 ** -15) * h64.abs() + (2.0 ** -8 * h64.abs() if dtype == BF16 else 0.0) + 2.0 ** -150).all()
+    if kw:
+        check_8bit(kw["h8"], kw["h8_scale"], h64, d)
