@@ -6,10 +6,11 @@
 //   g = softmax of z over S,  y = sum_k g_k W_down,k (silu(W_gate,k x) * (W_up,k x)).
 //
 // Five launches: logits, the selection with the plan of the experts' work (above 32
-// tokens a launch each), W_gate and W_up, W_down, the gated sum.  Or three, for one token and for a few that
-// hardly share an expert (each_alone): logits, W_gate and W_up with the selection
-// in front, W_down with the gated sum behind.  A small launch in between takes 4.5
-// us, whatever it does; joins within a launch (the last workgroup to arrive goes
+// tokens a launch each), W_gate and W_up, W_down, the gated sum.  Or three, for one
+// token and for a few that hardly share an expert (each_alone): logits, W_gate and
+// W_up with the selection in front, W_down with the gated sum behind.  A small launch
+// that reads what the one before it wrote takes 4.5 us, whatever it does (2.7 where
+// nothing was written just before); joins within a launch (the last workgroup to arrive goes
 // on) took more, 8 to 36 us: an atomic on one address takes 7 to 11 ns, a fence
 // for other workgroups 4 to 8 us.
 //
@@ -875,14 +876,20 @@ void launch_route(const MoeArgs& a, hipStream_t st) {
 // Few tokens of many experts: hardly two of them share one, and the plan's and the
 // gated sum's launches take longer than reading a shared expert's weights twice, as
 // long as the weights are not so many that the tiles of the joint launches stream
-// them faster.  Each alone against joint, us a call (top-8 of 128, 2048 x 768): bf16,
-// 2, 3 and 4 tokens (151, 226, 302 MB) 34.8 / 39.5, 47.9 / 50.9, 59.8 / 61.5; 8 bits
-// (78, 117, 156 MB) 25.3 / 33.2, 37.9 / 37.5, 42.4 / 41.2; top-6 of 256, 1024 x 512,
-// 4 tokens 24.1 / 32.9 and 19.5 / 29.8; 4096 x 1536, bf16, 4 tokens 198 / 186.
+// them faster.  Joint / each alone, us a layer, through so many layers that every
+// weight comes from HBM (MB: of the weights of all rows):
+//   top-8 of 128, 2048 x 768    bf16: 1 to 4 tokens (76 to 302 MB) 29.0 / 22.5, 40.1 / 36.5, 50.9 / 50.6, 60.5 / 60.3
+//                             8 bits: 1 to 4 (38 to 151 MB) 26.4 / 20.5, 32.0 / 27.1, 37.5 / 40.7, 42.3 / 47.3
+//                               fp32: 1 to 4 (151 to 604 MB) 42.2 / 38.7, 63.7 / 64.8, 89.8 / 91.8, 109 / 114
+//   top-6 of 256, 1024 x 512, 4 tokens  bf16 31.9 / 24.5, 8 bits 29.7 / 23.2, fp32 41.8 / 39.9 (75, 38, 151 MB)
+//   top-8 of 128, 4096 x 1536   bf16: 1, 2, 4 (302, 604, 1208 MB) 63.5 / 58.3, 105 / 104, 177 / 193
+//                             8 bits: 1, 2 (151, 302 MB) 45.2 / 41.3, 68.6 / 72.7; fp32: 1, 2 (604, 1208 MB) 119 / 119, 209 / 224
+//   top-4 of 32, 2880 x 2880, 1 token   bf16 45.9 / 45.1, 8 bits 39.2 / 34.4, fp32 80.5 / 86.0 (199, 100, 398 MB)
 bool each_alone(const MoeArgs& a) {
     const int64_t rows = (int64_t)a.T * a.K, values = rows * 3 * a.d * a.F;
     const int64_t bytes = a.format == kMoeMx8 ? values : a.format == kMoeBf16 ? 2 * values : 4 * values;
-    return a.T == 1 || (a.T <= 4 && 4 * rows <= a.N && bytes <= (a.format == kMoeMx8 ? 96 : 256) * 1000000ll);
+    const bool few = bytes <= (a.format == kMoeMx8 ? 96 : 256) * 1000000ll;
+    return a.T == 1 ? few || a.format != kMoeF32 : few && a.T <= 4 && 4 * rows <= a.N;
 }
 
 // The two products, with their variants for rows of whole lines or not.

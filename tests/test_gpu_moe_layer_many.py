@@ -144,3 +144,18 @@ def test_the_last_norm_behind_the_layers(kind, T):
     assert torch.equal(res.cpu(), r) and not torch.equal(r, before)
     check_h(h, h64, d, m.dtype)
     check_8bit(q, s, h64, d)
+
+
+def test_one_fp32_token_of_large_experts():
+    """Experts so large that one token too takes the launches for many."""
+    N, K, d, F, T = 5, 4, 2880, 1920, 1
+    m = Model("f32", 1, N, K, d, F, T, "one large", sigma=0.02)
+    layers, h = m.layers(), m.hidden(T)
+    y, sel, gates = outputs(T, K, d)
+    for n in (0, 1):
+        layers.cmoe_moe_layer(0, h.cuda(), y, selected=sel, gates=gates, n_tokens=torch.tensor([n], dtype=torch.int32, device="cuda"))
+        if n == 0:
+            assert (y == 7).all() and (sel == -9).all() and (gates == 9).all()
+    want = m.expected(0, h, h.double())
+    check((y, sel, gates), want, K)
+    assert rms_error(y.cpu(), want[2]) <= rms_bound(d, F, K)
