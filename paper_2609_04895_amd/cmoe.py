@@ -487,7 +487,9 @@ class MoeLayers:
     are the caller's tensors: w_router [L][N][d], logit_bias [L][N] fp32 or
     None, experts [L][N][3 d F] (expert_scales [L][N][3 d F / 32] with 8-bit
     ones), norm_weight [L][d] or None (ones) for cmoe_moe_block.  All calls run
-    on `stream` (default: the stream that is current here)."""
+    on `stream` (default: the stream that is current here).  Where a call's
+    tensors belong to another stream, the caller lets the two wait for each other
+    and keeps the tensors until the call is done (or calls their record_stream)."""
 
     def __init__(self, cfg: cmoe_moe_config, w_router, logit_bias, experts, expert_scales=None, norm_weight=None,
                  norm_eps=1e-6, stream=None):
@@ -515,6 +517,9 @@ class MoeLayers:
         self.stream = stream if stream is not None else torch.cuda.current_stream()
         with torch.cuda.stream(self.stream):  # the allocator's owner of the memory: the stream that uses it
             self.workspace = torch.empty(size, dtype=torch.uint8, device="cuda")
+        for t in (w_router, logit_bias, experts, expert_scales, None if norm_weight is None else norm_weight[0]):
+            if t is not None:  # once dropped, memory of the weights waits for the calls in flight
+                t.record_stream(self.stream)
         h = ctypes.c_void_p()
         _check(lib().cmoe_moe_init(ctypes.byref(cfg), ctypes.byref(w), self.workspace.data_ptr(),
                                    self.stream.cuda_stream, ctypes.byref(h)))
