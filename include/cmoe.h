@@ -401,8 +401,9 @@ typedef enum {
 } cmoe_format;
 
 /* Shape of L MoE layers run without caches.  1 <= K <= N.  Supported: N <= 256,
- * K <= 64, d and F multiples of 64 up to 65536, T <= 64 (cmoe_step takes larger
- * batches).  8-bit activations go with 8-bit weights. */
+ * K <= 64, d and F multiples of 64 up to 65536, T <= 64 (larger batches go in
+ * several calls; cmoe_step takes them in one, but no 8-bit pool).  8-bit activations
+ * go with 8-bit weights. */
 typedef struct {
     int32_t L, N, K, d, F;
     int32_t T;           /* tokens of a call, at most                             */

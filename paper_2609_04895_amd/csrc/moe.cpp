@@ -138,7 +138,7 @@ cmoe_status check_moe(const cmoe_moe_config* c) {
     for (int32_t f : {c->weights, c->activations})
         if (f != CMOE_FORMAT_DTYPE && f != CMOE_FORMAT_MX8) return fail(CMOE_ERR_INVALID_ARG, "unknown format");
     if (c->T > cmoe::kMoeTokens)
-        return fail(CMOE_ERR_UNSUPPORTED, "T > %d is not supported: cmoe_step takes larger batches", cmoe::kMoeTokens);
+        return fail(CMOE_ERR_UNSUPPORTED, "T > %d is not supported: larger batches go in several calls", cmoe::kMoeTokens);
     if (c->N > cmoe::kMaxN) return fail(CMOE_ERR_UNSUPPORTED, "N > 256 is not supported");
     if (c->K > cmoe::kMaxK) return fail(CMOE_ERR_UNSUPPORTED, "K > 64 is not supported");
     if (c->d % 64 || c->F % 64) return fail(CMOE_ERR_UNSUPPORTED, "d and F must be multiples of 64");

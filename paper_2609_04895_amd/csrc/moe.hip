@@ -757,23 +757,19 @@ __device__ __forceinline__ Tiles down_tiles(const MoeArgs& a, int expert, int ro
 }
 
 // Down projection and gated sum of a token: a workgroup takes a tile of outputs,
-// its wavefronts a part of an expert's sum each, `split` parts.  Half tiles, which
-// give all CUs a workgroup at d = 2048, for weights of 16 and 32 bits (2048 x 768
-// bf16, eight experts: 8.5 us against 9.8 with whole ones), whole tiles for 8-bit
-// weights, of which half tiles put too few bytes in flight (2880 x 2880, four
-// experts, nontemporal: 14.3 us against 16.6).
+// its wavefronts a part of an expert's sum each, `split` parts.  HALF: half tiles,
+// where whole ones leave many CUs without a workgroup (half_tiles).
 // grid: x = d / kTile, y = tokens
-template <int FORMAT>
+template <bool HALF>
 struct One {
-    static constexpr bool kHalf = !Format<FORMAT>::kScaled;
-    static constexpr int kTile = kHalf ? 8 : 16, kThreads = kHalf ? 512 : 1024, kWaves = kThreads / 64;
+    static constexpr int kTile = HALF ? 8 : 16, kThreads = HALF ? 512 : 1024, kWaves = kThreads / 64;
 };
 
-template <int FORMAT>
-__global__ __launch_bounds__(One<FORMAT>::kThreads) void moe_down_one_kernel(MoeArgs a, int split) {
+template <int FORMAT, bool HALF>
+__global__ __launch_bounds__(One<HALF>::kThreads) void moe_down_one_kernel(MoeArgs a, int split) {
     using P = Format<FORMAT>;
-    using O = One<FORMAT>;
-    __shared__ __align__(16) char lds[O::kWaves][kLineBytes<FORMAT, 1, 1, O::kHalf>];
+    using O = One<HALF>;
+    __shared__ __align__(16) char lds[O::kWaves][kLineBytes<FORMAT, 1, 1, HALF>];
     __shared__ __align__(16) float red[kMaxK][O::kTile];  // K split is at most kWaves, or K
     __shared__ float gate[kMaxK];                         // its product of an expert that is not selected is 0
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -790,7 +786,7 @@ __global__ __launch_bounds__(One<FORMAT>::kThreads) void moe_down_one_kernel(Moe
                                 ((int64_t)(first + k) * P::kPlanes + min(lane >> 3, P::kPlanes - 1)) * a.F * P::kBytes + (lane & 7) * 16};
             f32x4 acc[1][1] = {};
             const Tiles tiles = down_tiles<FORMAT>(a, unit.expert, blockIdx.x * O::kTile);
-            Product<FORMAT, 1, 1, O::kHalf>{tiles, x, P::kPlanes, part * lines / split, (part + 1) * lines / split, lines, lds[wv]}.run(acc);
+            Product<FORMAT, 1, 1, HALF>{tiles, x, P::kPlanes, part * lines / split, (part + 1) * lines / split, lines, lds[wv]}.run(acc);
             v = acc[0][0];
             if constexpr (P::kPlanes == 3)  // columns 0, 1, 2, the smallest first
 #pragma unroll
@@ -878,18 +874,18 @@ void launch_route(const MoeArgs& a, hipStream_t st) {
 // long as the weights are not so many that the tiles of the joint launches stream
 // them faster.  Joint / each alone, us a layer, through so many layers that every
 // weight comes from HBM (MB: of the weights of all rows):
-//   top-8 of 128, 2048 x 768    bf16: 1 to 4 tokens (76 to 302 MB) 29.0 / 22.5, 40.1 / 36.5, 50.9 / 50.6, 60.5 / 60.3
-//                             8 bits: 1 to 4 (38 to 151 MB) 26.4 / 20.5, 32.0 / 27.1, 37.5 / 40.7, 42.3 / 47.3
-//                               fp32: 1 to 4 (151 to 604 MB) 42.2 / 38.7, 63.7 / 64.8, 89.8 / 91.8, 109 / 114
-//   top-6 of 256, 1024 x 512, 4 tokens  bf16 31.9 / 24.5, 8 bits 29.7 / 23.2, fp32 41.8 / 39.9 (75, 38, 151 MB)
-//   top-8 of 128, 4096 x 1536   bf16: 1, 2, 4 (302, 604, 1208 MB) 63.5 / 58.3, 105 / 104, 177 / 193
-//                             8 bits: 1, 2 (151, 302 MB) 45.2 / 41.3, 68.6 / 72.7; fp32: 1, 2 (604, 1208 MB) 119 / 119, 209 / 224
-//   top-4 of 32, 2880 x 2880, 1 token   bf16 45.9 / 45.1, 8 bits 39.2 / 34.4, fp32 80.5 / 86.0 (199, 100, 398 MB)
+//   top-8 of 128, 2048 x 768    bf16: 1 to 4 tokens (76 to 302 MB) 28.4 / 22.5, 40.7 / 35.8, 51.6 / 52.3, 62.1 / 59.4
+//                             8 bits: 1 to 4 (38 to 151 MB) 26.3 / 20.6, 32.1 / 27.6, 37.6 / 40.2, 41.7 / 47.3
+//                               fp32: 1 to 4 (151 to 604 MB) 42.7 / 38.8, 63.6 / 58.8, 89.0 / 85.5, 107 / 106
+//   top-6 of 256, 1024 x 512, 4 tokens  bf16 32.0 / 24.2, 8 bits 29.5 / 23.3, fp32 41.8 / 35.8 (75, 38, 151 MB)
+//   top-8 of 128, 4096 x 1536   bf16: 1, 2, 4 (302, 604, 1208 MB) 62.5 / 57.7, 105 / 102, 188 / 192
+//                             8 bits: 1, 2 (151, 302 MB) 44.9 / 41.4, 67.5 / 73.1; fp32: 1, 2 (604, 1208 MB) 118 / 113, 207 / 211
+//   top-4 of 32, 2880 x 2880    bf16: 1, 2 (199, 398 MB) 46.2 / 42.8, 75.2 / 76.5; 8 bits: 1, 2 (100, 199 MB) 38.9 / 34.4, 56.3 / 57.3
+//                               fp32: 1, 2 (398, 796 MB) 79.0 / 76.2, 135 / 151
 bool each_alone(const MoeArgs& a) {
     const int64_t rows = (int64_t)a.T * a.K, values = rows * 3 * a.d * a.F;
     const int64_t bytes = a.format == kMoeMx8 ? values : a.format == kMoeBf16 ? 2 * values : 4 * values;
-    const bool few = bytes <= (a.format == kMoeMx8 ? 96 : 256) * 1000000ll;
-    return a.T == 1 ? few || a.format != kMoeF32 : few && a.T <= 4 && 4 * rows <= a.N;
+    return a.T == 1 || (a.T <= 4 && 4 * rows <= a.N && bytes <= (a.format == kMoeMx8 ? 96 : 512) * 1000000ll);
 }
 
 // The two products, with their variants for rows of whole lines or not.
@@ -898,13 +894,20 @@ void launch_up(const MoeArgs& a, int units, hipStream_t st) {
     launch_kernel(moe_up_kernel<FORMAT, RT, EACH>, dim3(a.F / (8 * RT), units), dim3(kThreads), st, Timing{}, a);
 }
 
-template <int FORMAT>
+// Half tiles for weights of 16 and 32 bits and fewer than 160 whole ones.  Half / whole,
+// us a layer on cold weights, bf16 and fp32: 1 token of d = 1024 (64 tiles) 15.0 / 15.6
+// and 22.3 / 22.3, of 2048 (128) 22.5 / 23.8 and 37.5 / 38.7, of 2880 (180) 46.2 / 42.5 and
+// 86.9 / 78.9, of 4096 (256) 59.7 / 58.1 and 116 / 109.  Half tiles of 8-bit weights put
+// too few bytes in flight (2880 x 2880, four experts: the launch 14.3 us against 16.6).
+bool half_tiles(const MoeArgs& a) { return a.format != kMoeMx8 && a.d / 16 * a.T < 160; }
+
+template <int FORMAT, bool HALF>
 void launch_down_one(const MoeArgs& a, hipStream_t st) {
-    using O = One<FORMAT>;
+    using O = One<HALF>;
     const int lines = (a.F + Format<FORMAT>::kLine - 1) / Format<FORMAT>::kLine;
     int split = 1;
     while (2 * split * a.K <= O::kWaves && 2 * split <= lines) split *= 2;
-    launch_kernel(moe_down_one_kernel<FORMAT>, dim3(a.d / O::kTile, a.T), dim3(O::kThreads), st, Timing{}, a, split);
+    launch_kernel(moe_down_one_kernel<FORMAT, HALF>, dim3(a.d / O::kTile, a.T), dim3(O::kThreads), st, Timing{}, a, split);
 }
 
 template <int FORMAT, int RT>
@@ -924,7 +927,13 @@ void launch_experts(const MoeArgs& a, hipStream_t st) {
     const int rows = a.T * a.K, units = moe_max_units(rows, a.N);
     if (each_alone(a)) {
         launch_up<UP, 1, true>(a, rows, st);
-        launch_down_one<DOWN>(a, st);
+        if constexpr (!Format<DOWN>::kScaled) {
+            if (half_tiles(a)) {
+                launch_down_one<DOWN, true>(a, st);
+                return;
+            }
+        }
+        launch_down_one<DOWN, false>(a, st);
         return;
     }
     if (a.T > 2 * kPlanThreads / 64) {

@@ -147,7 +147,7 @@ def test_the_last_norm_behind_the_layers(kind, T):
 
 
 def test_one_fp32_token_of_large_experts():
-    """Experts so large that one token too takes the launches for many."""
+    """One token of 265 MB of fp32 experts."""
     N, K, d, F, T = 5, 4, 2880, 1920, 1
     m = Model("f32", 1, N, K, d, F, T, "one large", sigma=0.02)
     layers, h = m.layers(), m.hidden(T)
@@ -159,3 +159,20 @@ def test_one_fp32_token_of_large_experts():
     want = m.expected(0, h, h.double())
     check((y, sel, gates), want, K)
     assert rms_error(y.cpu(), want[2]) <= rms_bound(d, F, K)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K,d,T", [(24, 3, 2496, 1), (24, 3, 2560, 1), (24, 3, 1216, 2), (24, 3, 1280, 2), (48, 3, 640, 4), (48, 3, 576, 4)])
+def test_tokens_alone_on_half_and_on_whole_tiles(kind, N, K, d, T):
+    """Both sides of 160 tiles of outputs, where the down product's tiles change."""
+    F = 192
+    m = Model(kind, 1, N, K, d, F, T, f"tiles {kind} {d} {T}", sigma=0.02)
+    layers, h = m.layers(), m.hidden(T)
+    y, sel, gates = outputs(T, K, d)
+    layers.cmoe_moe_layer(0, h.cuda(), y, selected=sel, gates=gates)
+    want = m.expected(0, h, h.double())
+    check((y, sel, gates), want, K)
+    assert rms_error(y.cpu(), want[2]) <= rms_bound(d, F, K)
+    y2, _, _ = outputs(T, K, d)
+    layers.cmoe_moe_layer(0, h.cuda(), y2, n_tokens=torch.tensor([T - 1], dtype=torch.int32, device="cuda"))
+    assert torch.equal(y2[:T - 1], y[:T - 1]) and (y2[T - 1:] == 7).all()
