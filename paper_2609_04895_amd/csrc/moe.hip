@@ -10,9 +10,9 @@
 // token and for a few that hardly share an expert (each_alone): logits, W_gate and
 // W_up with the selection in front, W_down with the gated sum behind.  A small launch
 // that reads what the one before it wrote takes 4.5 us, whatever it does (2.7 where
-// nothing was written just before); joins within a launch (the last workgroup to arrive goes
-// on) took more, 8 to 36 us: an atomic on one address takes 7 to 11 ns, a fence
-// for other workgroups 4 to 8 us.
+// nothing was written just before); joins within a launch (the last workgroup to
+// arrive goes on) took more, 8 to 36 us: an atomic on one address takes 7 to 11 ns, a
+// fence for other workgroups 4 to 8 us.
 //
 // The experts' weights are nearly all there is to read: 1 to 64 tokens use each
 // of them for a handful of products.  So everything is made for their stream.
@@ -21,16 +21,17 @@
 // into its operand registers, sixteen lines per instruction and 16 bytes of each,
 // the same stream runs at 5.0 instead of 6.8 TB/s (800 MB; a plain read of it runs
 // at 7.1).  The registers hold the lines in flight, not LDS (loads that go there
-// directly): 13.1 against 11.3 us for the gate and up products of one token's eight
-// experts, 302 against 268 us for those of 64 tokens in 8 bits.
+// directly): 302 against 268 us for the gate and up products of 64 tokens in 8 bits,
+// 13.1 against 11.3 for those of one token's eight experts out of the last-level cache.
 //
-// Medians, us, of one call (N x d x F, top-K, tokens; TB/s of the weights):
+// Medians, us, of one call on weights that come from HBM (N x d x F, top-K, tokens;
+// TB/s of the weights; plan: with the selection's launch):
 //                                  logits plan    up          down      sum
-//   128 x 2048 x 768, 8, bf16,  1    2.8         12.2 (4.1)   8.2 (3.1)
-//   128 x 2048 x 768, 8, bf16, 61    7.1   9.5  110   (6.7)  63.5 (5.8)  4.8
-//   128 x 2048 x 768, 8, 8 bit, 5    4.5   5.4   20.4 (5.6)  14.5 (3.9)  4.5
-//    32 x 2880 x 2880, 4, bf16, 16   4.6   5.4  142   (6.6)  73.5 (6.4)  4.6
-//   128 x 4096 x 1536, 8, 8 bit, 64  7.1   9.5  274   (6.0) 162   (5.1)  4.6
+//   128 x 2048 x 768, 8, bf16,  1    3.0         12.5 (4.0)   8.6 (2.9)
+//   128 x 2048 x 768, 8, bf16, 61    5.6   9.7  112   (6.6)  64.3 (5.7)  4.9
+//   128 x 2048 x 768, 8, 8 bit, 5    4.6   5.2   21.2 (5.4)  15.2 (3.8)  4.6
+//    32 x 2880 x 2880, 4, bf16, 16   4.7   4.8  140   (6.6)  70.3 (6.6)  4.7
+//   128 x 4096 x 1536, 8, 8 bit, 64  8.6   9.8  268   (6.1) 163   (5.0)  5.0
 // (rates: of the weights of the experts that the tokens reach.)
 #include <algorithm>
 

@@ -7,7 +7,7 @@
 // output written once.  Both kernels are bound by HBM for many rows (8192 rows of
 // 2880 bf16 values with an fp32 delta: 47.7 us, 5.5 TB/s; 604 million values into 8
 // bits: 294 us, 6.2 TB/s) and by the launch and one trip to memory for few (one row
-// of 2048: 2.6 us).
+// of 2048: 2.7 us).
 //
 // r is rounded to the residual's type before it is squared, so that the norm is
 // that of the residual as stored.  Squares, their sum and the factor are fp64, and r w
