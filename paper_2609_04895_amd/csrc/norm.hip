@@ -138,15 +138,18 @@ struct Factor {
     float hi, lo;
     __device__ Factor(double sum, const NormArgs& a) {
         const double s = 1.0 / sqrt(sum / a.d + (double)a.eps);
-        const bool normal = s > 0.0 && s < INFINITY;  // not of a row of zeros without an eps, of infinities or a NaN
-        e = normal ? ilogb(s) : 0;
+        // not of a row of zeros without an eps, of infinities or a NaN, whose finite
+        // values a power below all of them takes out of the product
+        const bool normal = s > 0.0 && s < INFINITY;
+        e = normal ? ilogb(s) : -512;
         const double m = ldexp(s, -e);
         hi = (float)m;
         lo = normal ? (float)(m - (double)hi) : 0.0f;
     }
     __device__ float times(float r, float w) const {
         const float v = ldexpf(r, e), p = v * w;
-        return __builtin_fmaf(p, hi, BF16 ? p * lo : __builtin_fmaf(p, lo, __builtin_fmaf(v, w, -p) * hi));
+        const float rest = BF16 ? p * lo : __builtin_fmaf(p, lo, __builtin_fmaf(v, w, -p) * hi);
+        return __builtin_fmaf(p, hi, fabsf(p) < INFINITY ? rest : 0.0f);  // h beyond fp32 is p's infinity
     }
 };
 

@@ -76,3 +76,27 @@ def test_norm_launch_shapes(rows, d, dtype):
     assert (off <= 2.0 ** -24 * (1 + 2.0 ** -15) * h64.abs() + (2.0 ** -8 * h64.abs() if dtype == BF16 else 0.0) + 2.0 ** -150).all()
     if kw:
         check_8bit(kw["h8"], kw["h8_scale"], h64, d)
+
+
+@pytest.mark.parametrize("rows,d", [(7, 64), (1030, 256), (5, 2880), (3, 50), (4, 8192)])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_norm_infinities(rows, d, dtype):
+    """An h beyond the type is infinite, so is one of an infinite weight; in a row with
+    an infinity the finite places are 0, whatever their weights."""
+    from paper_2609_04895_amd import cmoe as B
+    g = torch.Generator().manual_seed(rows + d)
+    res = (torch.randn((rows, d), generator=g) * torch.exp2(torch.arange(rows).float().remainder(40) - 20).unsqueeze(1)).to(dtype)
+    res[:, 0], res[:, 1] = 0.0, res[:, 2] * 8  # a zero and a place with a large h
+    res[2, 5], res[2, 7] = float("inf"), 2.0 ** 126
+    w = torch.ones(d).to(dtype)
+    w[1], w[7], w[9], w[11] = -2.0 ** 126, 2.0 ** 100, float("inf"), -float("inf")
+    h = torch.empty_like(res, device="cuda")
+    B.cmoe_add_norm(res.cuda(), None, w.cuda(), 2.0 ** -20, h=h)
+    want = ref.norm(res, None, w, 2.0 ** -20)[1]
+    got = h.cpu().double()
+    largest = torch.finfo(dtype).max
+    assert (want.abs() > 2 * largest).any() and torch.equal(got.isnan(), want.isnan())
+    beyond, within = want.abs() > largest * (1 + 2.0 ** -8), want.abs() <= largest * (1 - 2.0 ** -7)
+    assert (got[beyond].isinf() & (got[beyond].sign() == want[beyond].sign())).all()
+    assert ((got - want).abs()[within] <= (2.0 ** -8 if dtype == BF16 else 2.0 ** -24) * (1 + 2.0 ** -14) * want.abs()[within]).all()
+    assert (got[2][torch.isfinite(res[2]) & torch.isfinite(w)] == 0).all()
