@@ -356,8 +356,8 @@ cmoe_status cmoe_read_probe(const void* src, int64_t bytes, int32_t reps, double
  *   h = r / sqrt(mean(r^2) + eps) * weight
  * r is added in fp32 and rounded to dtype, stored to residual_out and normalised as
  * stored; squares, sums and the root are fp64; h is rounded to fp32 once, whatever
- * the sizes of r, weight and eps, and from there to dtype (h) and to 8 bits (h8,
- * h8_scale).
+ * the sizes of r, weight and eps (below 2^-100, to within two steps), and from there
+ * to dtype (h) and to 8 bits (h8, h8_scale).
  * Between two layer steps delta is the y of cmoe_step or cmoe_moe_layer, and h
  * the next layer's hidden states: strides let both be rows of [S][L][d].
  * Strides count values (h8 and h8_scale: bytes) and are at least the row.
