@@ -496,9 +496,9 @@ cmoe_status cmoe_quantize_as(int32_t format, const void* src, int32_t dtype, int
 
 /* y[t] = W x[t] for up to 64 rows of x (more are a cmoe_grouped_product of one group),
  * W in 4 bits: a projection or a vocabulary's logits while decoding.  Sums are fp32,
- * y is rounded once; an fp32 x is taken whole.  Outputs behind column m and rows behind
- * *n_rows are left as they were.  Rows of x and w are 16-byte aligned, d is a multiple
- * of 32 up to 2^18, m at most 2^24; y overlaps no input. */
+ * y is rounded once; an fp32 x is taken whole, but for what lies below 2^-133.  Outputs
+ * behind column m and rows behind *n_rows are left as they were.  Rows of x and w are
+ * 16-byte aligned, d is a multiple of 32 up to 2^18, m at most 2^24; y overlaps no input. */
 typedef struct {
     int32_t rows, m, d;
     int32_t dtype;              /* cmoe_dtype of x                                 */

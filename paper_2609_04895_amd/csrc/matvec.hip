@@ -5,7 +5,7 @@
 // kernels are streams of them.  A tile is 16 weight rows by up to 16 rows of x: lane (r, q)
 // = 16 q + r has 16 bytes, a block of 32 values, of weight row r, makes bf16 of them, scale
 // and all, and the bf16 matrix core multiplies; an fp32 x is the sum of three bf16
-// numbers (exactly but for the last bit or two).
+// numbers, exactly but for what lies below 2^-133, the smallest of them.
 #include <algorithm>
 
 #include "product.h"
@@ -16,9 +16,12 @@ namespace {
 
 constexpr int kLine = 256;  // values of 128 bytes of weights
 
+// The first part of a finite number is cut off, not rounded: of the largest ones the nearest
+// bf16 number would be infinity.  What is left has 16 bits, and the second part's rest 8.
 __device__ inline void split3(float v, __bf16* p) {
-    p[0] = (__bf16)v;
-    const float r = fabsf((float)p[0]) < INFINITY ? v - (float)p[0] : 0.0f;
+    const bool finite = fabsf(v) < INFINITY;
+    const float top = finite ? __uint_as_float(__float_as_uint(v) & 0xFFFF0000u) : v, r = finite ? v - top : 0.0f;
+    p[0] = (__bf16)top;
     p[1] = (__bf16)r;
     p[2] = (__bf16)(r - (float)p[1]);
 }
