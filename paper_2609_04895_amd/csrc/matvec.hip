@@ -42,6 +42,16 @@ __device__ __forceinline__ f32x4 multiply(const u32x4& w, uint32_t byte, const u
     return c;
 }
 
+// fp32 rows, whose products are added up three times as often and to more bits: a line of
+// 256 values is a chain of its own.  y off by, rms, for 4096 values 1.6e-7 in the wide kernel,
+// in one chain 5.5e-7; for 65536, 3.4e-7 and 2.1e-6, in the narrow one 1.9e-7 and 5.7e-7.  At
+// 131072 x 4096, 1 and 21 fp32 rows, 55.0 and 134 us, without 53.7 and 132; 2880 x 4096, 16
+// rows, 13.1 both.
+__device__ __forceinline__ void end_chain(f32x4& sum, f32x4& chain) {
+    sum += chain;
+    chain = f32x4{};
+}
+
 // Columns j .. j + 3 of row t of y.
 __device__ __forceinline__ void put(const MatvecArgs& a, int64_t t, int64_t j, const f32x4& v) {
     const int64_t at = t * a.y_stride + j;
@@ -136,11 +146,14 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void matvec_narrow_kernel(Matvec
             v = next;
         }
     } else {  // registers for one line of fp32 values
+        f32x4 sum = {};
         for (int l = wv; l < lines; l += waves) {
             Line v;
             load(l, v);
             step(v);
+            end_chain(sum, acc);
         }
+        acc = sum;
     }
     red[wv][lane] = acc;
     __syncthreads();
@@ -161,12 +174,14 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void matvec_narrow_kernel(Matvec
 // 137 us.
 // G: groups of 16 rows of x.  WHOLE: rows of whole lines of memory, which are read once,
 // nontemporally; elsewhere the caches keep a line's other part (46 us against 53.5).
+// fp32 rows: registers for four wavefronts a SIMD, two workgroups a CU; left to itself the
+// compiler takes 139 for two tiles, and 131072 x 4096 takes 56.2 us instead of 55.0.
 // grid: x = tiles / (RT kWaves) rounded up
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kXBytes = 32 * 1024;  // of LDS for x
 
 template <int PLANES, int RT, int G, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void matvec_wide_kernel(MatvecArgs a, int columns, int chunk) {
+__global__ __launch_bounds__(kThreads, PLANES == 3 ? 4 : 1) void matvec_wide_kernel(MatvecArgs a, int columns, int chunk) {
     constexpr int kMine = (kXBytes / (PLANES * 16) + kThreads - 1) / kThreads;  // blocks of eight values of a chunk, per thread
     __shared__ __align__(16) char xs[kXBytes];
     __shared__ __align__(16) char ws[kWaves][RT * 2048];
@@ -256,7 +271,7 @@ __global__ __launch_bounds__(kThreads) void matvec_wide_kernel(MatvecArgs a, int
         load(0, v);
         load_scales(0, s);
     }
-    f32x4 acc[RT][G] = {};
+    f32x4 acc[RT][G] = {}, sum[RT][G] = {};
     char* const lds = ws[wv];
     for (int c0 = 0; c0 < lines; c0 += chunk) {
         const int c1 = min(c0 + chunk, lines);
@@ -307,6 +322,11 @@ __global__ __launch_bounds__(kThreads) void matvec_wide_kernel(MatvecArgs a, int
                     }
                 }
             }
+            if constexpr (PLANES == 3)
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int g = 0; g < G; ++g) end_chain(sum[t][g], acc[t][g]);
             __builtin_amdgcn_wave_barrier();
         }
     }
@@ -316,7 +336,7 @@ __global__ __launch_bounds__(kThreads) void matvec_wide_kernel(MatvecArgs a, int
     for (int t = 0; t < RT; ++t)
 #pragma unroll
         for (int g = 0; g < G; ++g)
-            if (16 * g + r < n) put(a, a.row0 + 16 * g + r, (int64_t)(tile0 + t) * 16 + 4 * q, acc[t][g]);
+            if (16 * g + r < n) put(a, a.row0 + 16 * g + r, (int64_t)(tile0 + t) * 16 + 4 * q, PLANES == 3 ? sum[t][g] : acc[t][g]);
 }
 
 template <int PLANES, int RT, int G>

@@ -10,19 +10,20 @@ import math
 
 import pytest
 
+import mx4_reference as mx
 from gpu_util import say, stable_seed
 
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-U = 2.0 ** -24
+F32, U8, U = torch.float32, torch.uint8, 2.0 ** -24
 
 
-def bound(d):
-    """Two more for y's own rounding and the join of wavefronts; a tenth for chance, over
-    4096 values and more."""
-    return 1.1 * U * math.sqrt((256 + d / 64) / 6 + 2)
+def bound(d, each=1):
+    """each: roundings per value.  Two more for y's own and the join of wavefronts; a tenth
+    for chance, over 4096 values and more."""
+    return 1.1 * U * math.sqrt((256 * each + d / 64) / 6 + 2)
 
 
 def close(y, want, most):
@@ -56,3 +57,26 @@ def test_grouped_products(sizes, m, d):
     # error counts sqrt((1.21 + 0.356) / 0.356) = 2.1 times; and the roundings of silu
     B.cmoe_grouped_product(x, w, first, y, swiglu=True)
     close(y, torch.nn.functional.silu(gate) * up, 2.1 * bound(d) + 4 * U)
+
+
+def dequantized(q, s):
+    table = torch.cat((mx.E2M1, -mx.E2M1)).cuda()
+    v = table[torch.stack((q & 15, q >> 4), -1).reshape(q.shape[0], -1).int()]
+    return (v.view(*s.shape, 32) * torch.pow(2.0, s.double() - 127).unsqueeze(-1)).view(v.shape)
+
+
+# few weight rows; many, one tile a wavefront; in two launches; two tiles a wavefront
+@pytest.mark.parametrize("rows,m,d", [(16, 256, 4096), (1, 4096, 2048), (8, 512, 65536), (16, 256, 1 << 18), (16, 10240, 4096), (25, 10240, 4096),
+                                      (16, 10240, 65536), (8, 131072, 512)])
+def test_matvec(rows, m, d):
+    """An fp32 x is three bf16 numbers: three products a value."""
+    from paper_2609_04895_amd import cmoe as B
+    say(f"fp32 sums matvec rows {rows} m {m} d {d}")
+    g = torch.Generator(device="cuda").manual_seed(stable_seed(f"sums mv {rows} {m} {d}"))
+    q = torch.randint(0, 256, (m, d // 2), dtype=U8, device="cuda", generator=g)
+    s = torch.randint(124, 128, (m, d // 32), dtype=U8, device="cuda", generator=g)
+    x = torch.empty((rows, d), device="cuda").normal_(generator=g)
+    y = torch.empty((rows, m), device="cuda")
+    B.cmoe_matvec(x, q, s, y)
+    some = torch.arange(m, device="cuda") if m <= 4096 else torch.randperm(m, device="cuda", generator=g)[:512]
+    close(y[:, some], x.double() @ dequantized(q[some], s[some]).t(), bound(d, 3))
