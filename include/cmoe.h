@@ -478,7 +478,10 @@ cmoe_status cmoe_moe_destroy(cmoe_moe* hd);
 
 /* ------------------------------------------------------------------------
  * Operators that take an expert pool beyond a few tokens and beyond 8 bits.  They
- * share the conventions of the operators above.
+ * share the conventions of the operators above.  Outputs that overlap an input are
+ * refused; columns of one buffer, and values with their scales behind them in a row's
+ * record, do not overlap.  (Of two tensors whose rows are at different distances the
+ * stretches from the first byte to the last have to be apart.)
  *
  * 4-bit values: e2m1 numbers (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives), two to
  * a byte, the first in the low half, with one power-of-two scale 2^E for every 32

@@ -8,6 +8,7 @@
 #include <new>
 
 #include "checks.h"
+#include "places.h"
 
 namespace {
 
@@ -24,29 +25,6 @@ int64_t held_bytes(int format, int dtype, int64_t n) {
 // Strides that no memory has room for, and that the products below have no bits for.
 bool beyond(std::initializer_list<int64_t> strides) {
     return std::any_of(strides.begin(), strides.end(), [](int64_t s) { return s > (int64_t)1 << 48; });
-}
-
-// A stretch of memory from p: rows, `pitch` bytes apart, of `row` bytes.
-struct Span {
-    const void* p;
-    int64_t rows, pitch, row;
-    using Address = unsigned __int128;
-    Address begin() const { return reinterpret_cast<uintptr_t>(p); }
-    Address end() const { return begin() + (Address)(rows - 1) * (Address)pitch + (Address)row; }
-    bool empty() const { return !p || rows <= 0 || row <= 0; }
-};
-
-// Whether no output has memory between the first and the last byte of an input or of
-// another output.
-bool apart(std::initializer_list<Span> outputs, std::initializer_list<Span> inputs) {
-    auto meet = [](const Span& a, const Span& b) { return !a.empty() && !b.empty() && a.begin() < b.end() && b.begin() < a.end(); };
-    for (auto o = outputs.begin(); o != outputs.end(); ++o) {
-        for (const Span& i : inputs)
-            if (meet(*o, i)) return false;
-        for (auto p = outputs.begin(); p != o; ++p)
-            if (meet(*o, *p)) return false;
-    }
-    return true;
 }
 
 cmoe_status ready(void* stream) {
