@@ -578,7 +578,8 @@ cmoe_status cmoe_prompt_query(const cmoe_moe_config* cfg, size_t* workspace_byte
 cmoe_status cmoe_prompt_init(const cmoe_moe_config* cfg, const cmoe_moe_weights* w, void* workspace, void* stream,
                              cmoe_prompt** out);
 
-/* As cmoe_moe_call, but for y, which is in the configuration's dtype. */
+/* As cmoe_moe_call, but for y, which is in the configuration's dtype; outputs overlap no
+ * weight either, and nothing lies in the workspace. */
 typedef struct {
     int32_t layer;
     int32_t T;

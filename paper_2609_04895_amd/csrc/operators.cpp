@@ -170,11 +170,24 @@ Parts prompt_parts(const cmoe_moe_config* c) {
     return p;
 }
 
+// Where the weights of all layers lie, and the workspace.
+struct Held {
+    Span router, bias, experts, scales, workspace;
+};
+Held held(const cmoe_moe_config* c, const cmoe_moe_weights* w, const void* workspace) {
+    const Span::Bytes logits = static_cast<Span::Bytes>(c->L) * c->N, pool = logits * 3 * c->d * c->F;
+    auto flat = [](const void* p, Span::Bytes n) { return Span{p, 1, 0, static_cast<int64_t>(std::min<Span::Bytes>(n, INT64_MAX))}; };
+    return {flat(w->w_router, logits * c->d * elem(c->dtype)), flat(w->logit_bias, logits * 4),
+            flat(w->experts, c->weights == CMOE_FORMAT_MX4 ? pool / 2 : c->weights == CMOE_FORMAT_MX8 ? pool : pool * elem(c->dtype)),
+            flat(c->weights != CMOE_FORMAT_DTYPE ? w->expert_scales : nullptr, pool / 32), flat(workspace, prompt_parts(c).bytes)};
+}
+
 }  // namespace
 
 struct cmoe_prompt {
     cmoe_moe_config cfg;
     cmoe_moe_weights w;
+    Held at;
     Parts parts;
     char* ws;
     hipStream_t stream;
@@ -274,6 +287,9 @@ cmoe_status cmoe_prompt_init(const cmoe_moe_config* cfg, const cmoe_moe_weights*
     if (!workspace || !aligned_to(workspace, 256)) return fail(CMOE_ERR_INVALID_ARG, "a workspace is required, 256-byte aligned");
     if (!aligned_to(w->w_router, 16) || !aligned_to(w->experts, 16) || !aligned_to(w->logit_bias, 4))
         return fail(CMOE_ERR_INVALID_ARG, "w_router and experts must be 16-byte aligned, logit_bias 4-byte");
+    const Held at = held(cfg, w, workspace);
+    if (!apart({at.workspace}, {at.router, at.bias, at.experts, at.scales}))
+        return fail(CMOE_ERR_INVALID_ARG, "the workspace overlaps a weight");
     int device = 0;
     if ((st = current_device(&device)) != CMOE_OK) return st;
     if ((st = check_stream(static_cast<hipStream_t>(stream), device)) != CMOE_OK) return st;
@@ -291,6 +307,7 @@ cmoe_status cmoe_prompt_init(const cmoe_moe_config* cfg, const cmoe_moe_weights*
     if (!m) return fail(CMOE_ERR_UNSUPPORTED, "no host memory for the handle");
     m->cfg = *cfg;
     m->w = *w;
+    m->at = at;
     m->parts = prompt_parts(cfg);
     m->ws = static_cast<char*>(workspace);
     m->stream = static_cast<hipStream_t>(stream);
@@ -327,12 +344,13 @@ cmoe_status cmoe_prompt_layer(cmoe_prompt* m, const cmoe_prompt_call* c) {
     if (!aligned_to(c->n_tokens, 4) || !aligned_to(c->selected, 4) || !aligned_to(c->gates, 4))
         return fail(CMOE_ERR_INVALID_ARG, "a pointer is not aligned to its values");
     const int64_t picks = 4 * (int64_t)c->T * g.K;
-    if (!apart({{c->y, c->T, c->y_stride * e, g.d * e}, {c->selected, 1, 0, picks}, {c->gates, 1, 0, picks}},
+    if (!apart({m->at.workspace, {c->y, c->T, c->y_stride * e, g.d * e}, {c->selected, 1, 0, picks}, {c->gates, 1, 0, picks}},
                {{c->h, c->T, c->h_stride * e, g.d * e},
                 {c->h8, c->T, c->h8_stride, g.d},
                 {c->h8_scale, c->T, c->h8_scale_stride, g.d / 32},
-                {c->n_tokens, 1, 0, 4}}))
-        return fail(CMOE_ERR_INVALID_ARG, "an output overlaps an input or another output");
+                {c->n_tokens, 1, 0, 4},
+                m->at.router, m->at.bias, m->at.experts, m->at.scales}))
+        return fail(CMOE_ERR_INVALID_ARG, "an output or the workspace overlaps an input, a weight or an output");
 
     auto part = [m](size_t at) { return static_cast<void*>(m->ws + at); };
     cmoe::PromptArgs a{};
