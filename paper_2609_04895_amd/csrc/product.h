@@ -15,7 +15,6 @@
 
 namespace cmoe {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -831,7 +830,7 @@ struct FewRows {
                     if constexpr (kX8)
                         b = eight(v.x[h][j / 2], v.xs[h], j & 1);
                     else
-                        b = __builtin_bit_cast(bf16x8, v.x[h][kX8 ? 0 : j]);
+                        b = __builtin_bit_cast(bf16x8, v.x[h][j]);
 #pragma unroll
                     for (int t = 0; t < RT; ++t)
                         acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(weight(v.w[h][t], v.ws[h][t], j), b, acc[t], 0, 0, 0);

@@ -28,20 +28,13 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 
 __device__ inline int live_tokens(const PromptArgs& a) { return a.n_tokens ? min(max(*a.n_tokens, 0), a.T) : a.T; }
 
-template <bool BF16>
-__device__ inline void load8(const void* p, int64_t i, float* v) {
-    if constexpr (BF16) {
-        const bf16x8 r = *reinterpret_cast<const bf16x8*>(static_cast<const __bf16*>(p) + i);
+__device__ inline void load8(const float* p, float* v) {
+    const f32x4* s = reinterpret_cast<const f32x4*>(p);
+    const f32x4 a = s[0], b = s[1];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = (float)r[j];
-    } else {
-        const f32x4* s = reinterpret_cast<const f32x4*>(static_cast<const float*>(p) + i);
-        const f32x4 a = s[0], b = s[1];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v[j] = a[j];
-            v[4 + j] = b[j];
-        }
+    for (int j = 0; j < 4; ++j) {
+        v[j] = a[j];
+        v[4 + j] = b[j];
     }
 }
 
@@ -274,7 +267,7 @@ __global__ __launch_bounds__(kThreads) void prompt_sum_kernel(PromptArgs a) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = (float)h[i] * s;
         } else {
-            load8<false>(a.out, row * a.d + j, v);
+            load8(static_cast<const float*>(a.out) + row * a.d + j, v);
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] += g * v[i];
