@@ -488,7 +488,9 @@ cmoe_status cmoe_moe_destroy(cmoe_moe* hd);
  * consecutive values of a row, kept as the byte E + 127.  E is the smallest exponent,
  * -127 at least, with max |v| <= 6 2^E; each value is rounded once, to nearest even.
  * A block that holds an infinity or a NaN gets the byte 255, which stands for NaN in
- * all its places.
+ * all its places.  The products take 8-bit and 4-bit values as bf16 numbers or on the
+ * 8-bit core: a value of 2^128 or more, which only the largest scales give, may count as
+ * infinite, and one below 2^-133 as 0.
  */
 
 /* Rows of fp32 or bf16 values into 8 bits (CMOE_FORMAT_MX8: cmoe_quantize) or 4
@@ -528,8 +530,9 @@ cmoe_status cmoe_matvec(const cmoe_vectors* v, void* stream);
  * left as they were.  Where x_row[i] is no row of x, y[i] is 0.  Sums are fp32 and y is
  * rounded once.  With 8-bit rows of x and a bf16 y the 8-bit matrix core adds 32
  * products at a time with 13 bits below the largest of them, and the sums of 32 in fp32:
- * 1.5e-5 of a typical y, less than a hundredth of the rounding to bf16; a y in 8 bits
- * is rounded from fp32 sums, at half that rate; a y in fp32 is refused.
+ * 1.5e-5 of a typical y, less than a hundredth of the rounding to bf16, and where products
+ * cancel up to 2^-7 of the largest of each 32; a y in 8 bits is rounded from fp32 sums, at
+ * half that rate; a y in fp32 is refused.
  * x and w: in dtype, or with the bf16 type w in 8 or 4 bits, x in 8 (with such w).
  * N <= 256, rows <= 2^22, m <= 2^18, d a multiple of 64 up to 65536.  Rows of x and
  * matrices of w are 16-byte aligned, the rows of a matrix follow each other; y

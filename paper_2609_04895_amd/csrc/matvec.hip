@@ -171,7 +171,8 @@ __global__ __launch_bounds__(64 * kNarrowWaves) void matvec_narrow_kernel(Matvec
 // Bound by HBM: 131072 x 4096, one row of x, 47.3 us, 6.0 TB/s.  Rows that are no whole
 // lines of memory, 131075 x 2880, five rows, 44.2 us, 4.6 TB/s: a load of 128 bytes takes
 // parts of two lines there.  With 64 rows of x by x's reads from LDS: 131072 x 4096 in
-// 137 us.
+// 130 us.  A line of more than 21 fp32 rows does not fit into x's LDS, so they are launches
+// of 21, which read the weights each: 22 and 64 rows, 131072 x 4096, in 192 and 459 us.
 // G: groups of 16 rows of x.  WHOLE: rows of whole lines of memory, which are read once,
 // nontemporally; elsewhere the caches keep a line's other part (46 us against 53.5).
 // fp32 rows: registers for four wavefronts a SIMD, two workgroups a CU; left to itself the
@@ -355,10 +356,11 @@ void launch(const MatvecArgs& args, hipStream_t st) {
     const int64_t tiles = (args.m + 15) / 16;
     // A wavefront of the wide kernel goes through whole rows, which takes its time however few
     // there are; the narrow one's wavefronts share a row, but not x.  us, narrow / wide, bf16,
-    // 1 and 16 rows of x: m = 4096, d = 4096, 11.4 / 13.5 and 11.8 / 15.7; 8192, 12.1 / 13.8 and
-    // 16.3 / 16.2; 12288, 15.8 / 14.0 and 25.0 / 16.4; 32768, 27.3 / 15.7 and 54.3 / 18.3; d =
-    // 16384, m = 8192, 30.5 / 45.2 and 55.2 / 56.4; d = 2048, m = 8192, 14.4 / 8.5 and 10.5 / 9.4,
-    // 16384, 11.4 / 8.8 and 14.9 / 9.7; d = 4096, 64 rows, m = 2048, 15.6 / 34.1, 8192, 54.9 / 34.2.
+    // 1 and 16 rows of x: m = 4096, d = 4096, 6.8 / 13.2 and 8.3 / 15.3; 8192, 10.3 / 13.5 and
+    // 15.3 / 15.5; 12288, 13.5 / 13.7 and 21.1 / 15.9; 32768, 25.5 / 15.4 and 52.5 / 18.0; d =
+    // 16384, m = 8192, 29.2 / 45.1 and 53.5 / 56.0; d = 2048, m = 8192, 6.4 / 8.3 and 8.2 / 9.1,
+    // 10000, 7.8 / 8.3 and 10.8 / 9.1, 16384, 9.4 / 8.5 and 13.5 / 9.3; d = 4096, 64 rows, m =
+    // 2048, 15.0 / 30.6, 8192, 54.9 / 33.5.
     if (tiles * ((args.rows + 15) / 16) < 640) {
         // as many wavefronts as have a line each, unless the tiles alone are many
         const int waves = (int)std::min<int64_t>(std::min(kNarrowWaves, lines), std::max<int64_t>(2, 8192 / tiles));

@@ -914,7 +914,9 @@ void launch_product_held(const ProductArgs& a, hipStream_t st) {
     // Few rows of few groups leave most of the device without a tile.  us, tiles of 128 x 128
     // against few rows: 2048 x 2048 bf16, 1 group of 16 rows 21 / 12, 8 of 1 20 / 17, of 16 22 /
     // 36; 1536 x 2048, 64 groups of one row 71 / 83, 128 of 8 132 / 212; 8-bit weights 61 / 55
-    // and 104 / 136.
+    // and 104 / 136.  How rows spread over the groups is known on the device only: of 128 groups
+    // all 1000 rows in one, by 64 x 2048, bf16 23.2 / 12.5, 8-bit weights 27.0 / 10.6, but by 768
+    // x 2048, 8-bit weights 25.4 / 48.4, 4-bit ones 25.4 / 39.0.
     const int64_t scarce = HELD == kHeldSame ? 1 : 2;
     if ((rows <= 8 && middle < 512 * scarce) || (rows <= 32 && middle < 128 * scarce)) {
         launch_product_few<KIND, HELD>(a, st);
@@ -932,7 +934,9 @@ void launch_product_held(const ProductArgs& a, hipStream_t st) {
         // 126 / 142, 493 / 591, and 67 / 66, 104 / 100, 365 / 416; 8-bit rows with 4-bit weights 76 /
         // 67, 96 / 116, 421 / 465, and 62 / 51, 87 / 74, 314 / 320.  Where every wavefront widens
         // 4-bit weights, 134 / 114, 176 / 192, 512 rows 415 / 428, 1024 758 / 827, and 117 / 86, 160 /
-        // 132, 319 / 300, 547 / 572; of 32 x (5760 x 2880), 128 rows 203 / 201, 512 605 / 562.
+        // 132, 319 / 300, 547 / 572; of 32 x (5760 x 2880), 128 rows 203 / 201, 512 605 / 562: the
+        // small tile up to 768 rows there, which loses a tenth at most (192 rows of 2048 values)
+        // where the large one loses a fifth (192 of 2880).
         constexpr int64_t kLargeFrom = KIND == kProductBf16 && HELD == kHeld4 ? 768 : 28 * kMost;  // 7/8 of the small tile
         if (rows >= kLargeFrom && fills)
             launch_product_tile<KIND, HELD, 64, kMost, 256, 2, 4, 1>(a, st);
