@@ -198,23 +198,23 @@ extern "C" {
 
 cmoe_status cmoe_quantize_as(int32_t format, const void* src, int32_t dtype, int64_t rows, int64_t cols, int64_t src_stride, uint8_t* q,
                              int64_t q_stride, uint8_t* scale, int64_t scale_stride, void* stream) {
-    if (format == CMOE_FORMAT_MX8) return cmoe_quantize(src, dtype, rows, cols, src_stride, q, q_stride, scale, scale_stride, stream);
-    if (format != CMOE_FORMAT_MX4) return fail(CMOE_ERR_INVALID_ARG, "quantize: the format must be 8 or 4 bits");
+    if (format != CMOE_FORMAT_MX8 && format != CMOE_FORMAT_MX4) return fail(CMOE_ERR_INVALID_ARG, "quantize: the format must be 8 or 4 bits");
     if (rows < 0 || cols < 0) return fail(CMOE_ERR_INVALID_ARG, "quantize: rows and cols must be >= 0");
     if (!known_dtype(dtype)) return fail(CMOE_ERR_INVALID_ARG, "quantize: unknown dtype");
     if (cols % 32) return fail(CMOE_ERR_INVALID_ARG, "quantize: cols must be a multiple of 32");
     if (cols && rows > ((int64_t)1 << 34) / cols) return fail(CMOE_ERR_UNSUPPORTED, "quantize: more than 2^34 values");
     if (rows && cols) {
+        const int64_t e = (int64_t)elem(dtype), q_row = held_bytes(format, dtype, cols);
         if (!src || !q || !scale) return fail(CMOE_ERR_INVALID_ARG, "quantize: src, q and scale are required");
-        if (src_stride < cols || q_stride < cols / 2 || scale_stride < cols / 32)
+        if (src_stride < cols || q_stride < q_row || scale_stride < cols / 32)
             return fail(CMOE_ERR_INVALID_ARG, "quantize: a row stride is less than the row");
         if (beyond({src_stride, q_stride, scale_stride})) return fail(CMOE_ERR_UNSUPPORTED, "quantize: a stride of more than 2^48 is not supported");
-        const int64_t e = (int64_t)elem(dtype);
         if (!aligned_to(src, 16) || src_stride * e % 16 || !aligned_to(q, 16) || q_stride % 16)
             return fail(CMOE_ERR_UNSUPPORTED, "quantize: rows of src and q must be 16-byte aligned");
-        if (!apart({{q, rows, q_stride, cols / 2}, {scale, rows, scale_stride, cols / 32}}, {{src, rows, src_stride * e, cols * e}}))
+        if (!apart({{q, rows, q_stride, q_row}, {scale, rows, scale_stride, cols / 32}}, {{src, rows, src_stride * e, cols * e}}))
             return fail(CMOE_ERR_INVALID_ARG, "quantize: an output overlaps src or the other output");
     }
+    if (format == CMOE_FORMAT_MX8) return cmoe_quantize(src, dtype, rows, cols, src_stride, q, q_stride, scale, scale_stride, stream);
     const cmoe_status st = ready(stream);
     if (st != CMOE_OK || rows == 0 || cols == 0) return st;
     const cmoe::QuantizeArgs a{dtype == CMOE_BF16, src, rows, cols, src_stride, q, q_stride, scale, scale_stride};

@@ -106,3 +106,11 @@ def test_matvec_and_quantize_columns_that_meet_are_refused():
     for q, scale in ((P + 112, 3 * P), (2 * P, P + 127), (2 * P, 2 * P + 31), (P + 128, P + 159)):
         st = B.lib().cmoe_quantize_as(B.CMOE_FORMAT_MX4, P, B.CMOE_BF16, 4, 64, 128, q, 256, scale, 256, None)
         assert st == B.CMOE_ERR_INVALID_ARG and "overlaps" in error()
+
+
+def test_8_bit_rows_that_meet_their_source_are_refused_too():
+    for q, scale in ((P, 3 * P), (P + 112, 3 * P), (P - 48, 3 * P), (2 * P, P + 127), (2 * P, 2 * P + 63), (P + 128, P + 191)):
+        st = B.lib().cmoe_quantize_as(B.CMOE_FORMAT_MX8, P, B.CMOE_BF16, 4, 64, 128, q, 256, scale, 256, None)
+        assert st == B.CMOE_ERR_INVALID_ARG and "overlaps" in error()
+    st = B.lib().cmoe_quantize_as(B.CMOE_FORMAT_MX8, P, B.CMOE_BF16, 4, 64, (1 << 48) + 64, 2 * P, 64, 3 * P, 2, None)
+    assert st == B.CMOE_ERR_UNSUPPORTED and "2^48" in error()
